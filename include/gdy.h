@@ -306,6 +306,135 @@ gdy_status gdy_execute_static(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, in
                               int32_t forced_cd, void* hip_stream, gdy_plan_t* out);
 
 /*
+ * Epilogues: what a GEMM does with its fp32 sums before the one rounding into C.
+ *   z(i,j) = scale_a * scale_b * sum_k op(A)(i,k) op(B)(k,j) + bias(j)
+ *   forward  (grad = 0): C(i,j) = round(f(z) + R(i,j)); aux(i,j) = round(z) where
+ *                        aux is given (a backward pass reads it)
+ *   backward (grad = 1): C(i,j) = round(z * f'(aux(i,j)) + R(i,j)), aux the saved
+ *                        pre-activation (not read for GDY_ACT_NONE)
+ *   bias_grad(j) = the sum of column j of C before its rounding, in fp32 and in an
+ *                  order that the plan fixes: the gradient of the bias that the
+ *                  layer below added to aux.
+ * f: the identity, max(z, 0), z Phi(z) (the normal distribution function), z (1 +
+ * tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2, or z / (1 + exp(-z)).  The slope of
+ * GDY_ACT_RELU at 0 is 0.  A zeroed struct is no epilogue.
+ */
+typedef enum {
+  GDY_ACT_NONE = 0,
+  GDY_ACT_RELU = 1,
+  GDY_ACT_GELU = 2,
+  GDY_ACT_GELU_TANH = 3,
+  GDY_ACT_SILU = 4
+} gdy_act;
+
+typedef struct {
+  int32_t act;                      /* gdy_act                                              */
+  int32_t grad;                     /* 0: forward, 1: backward                              */
+  const void* bias;                 /* N values, or NULL                                    */
+  int32_t bias_type;                /* of bias: C's type or GDY_F32 (ignored without bias)  */
+  int32_t reserved;                 /* must be 0                                            */
+  const void* residual; int64_t ldr;    /* R: M x N of C's type, or NULL; ldr >= n          */
+  void* aux;            int64_t ldaux;  /* M x N of C's type, or NULL; ldaux >= n           */
+  float* bias_grad;                 /* N values, or NULL; overwritten                       */
+  /* between items of a strided batch (or groups, gdy_execute_grouped), in elements: bias 0
+   * shares one bias, bias_grad 0 adds the items' sums up.  Ignored for a single GEMM. */
+  int64_t stride_bias, stride_r, stride_aux, stride_bias_grad;
+} gdy_epilogue;
+
+/*
+ * gdy_execute for GEMMs with epilogues: epilogues[i] belongs to gemms[i] (a
+ * host array of n, read during the call only; NULL: no epilogues, exactly
+ * gdy_execute).  The plan is gdy_execute's for the same GEMMs, and every mode takes
+ * them; members with and without epilogues mix, and adds (GDY_OP_ADD) must have
+ * none.  R may be C itself (same pointer, ldr = ldc, stride_r = stride_c), as may
+ * a backward pass's aux; otherwise no output (C, a written aux, bias_grad) may
+ * overlap anything else that the submission reads or writes.  k = 0 gives z =
+ * bias; m = 0 writes nothing but a bias_grad of zeros.
+ * Every pointer is aligned to its elements.  The split-K workspace also holds the
+ * partial column sums of a group's bias gradients: a group that needs more of both
+ * than the workspace has is refused (GDY_ERR_UNSUPPORTED) before anything launches.
+ */
+gdy_status gdy_execute_epilogue(gdy_ctx* ctx, const gdy_gemm* gemms, const gdy_epilogue* epilogues, int32_t n,
+                                int32_t mode, int32_t forced_cd, void* hip_stream, gdy_plan_t* out);
+/* The same as gdy_execute_static is to gdy_execute: the workspace is the library's static array. */
+gdy_status gdy_execute_epilogue_static(gdy_ctx* ctx, const gdy_gemm* gemms, const gdy_epilogue* epilogues,
+                                       int32_t n, int32_t mode, int32_t forced_cd, void* hip_stream,
+                                       gdy_plan_t* out);
+
+/*
+ * Products grouped by expert (the GEMMs of a mixture-of-experts layer): independent
+ * products whose row counts only the device knows.  The rows of A are sorted by
+ * group; group e holds the rows [offsets[e], offsets[e+1]) (device array of groups
+ * + 1 values, not decreasing, 0 <= offsets[0], offsets[groups] <= rows; values outside
+ * 0 .. rows are clamped to it, so that no offset leads outside the operands).
+ *   GDY_OVER_ROWS: C[i][:] = epilogue(scale * A[i][:] op(B_e)) for the rows i of e:
+ *                  A rows x k, B_e k x n (trans_b: stored n x k), C rows x n.  The
+ *                  forward product, and with the other trans_b its input gradient.
+ *                  Rows of no group are left as they were.
+ *   GDY_OVER_K:    C_e = scale * A_e^T B_e + R_e, A_e and B_e the rows of e of A (rows
+ *                  x k) and B (rows x n), C_e k x n: the weight gradient.  A group
+ *                  without rows gives R_e or zeros.
+ * with scale = scale_a * scale_b * scales[e].  Types, storage, rounding and
+ * alignment as for gdy_gemm; several groups may share a B (stride_b 0).
+ */
+#define GDY_MAX_GROUPS 4096
+typedef enum { GDY_OVER_ROWS = 0, GDY_OVER_K = 1 } gdy_over;
+
+typedef struct {
+  int32_t over;                     /* gdy_over                                             */
+  int32_t groups;                   /* 0 .. GDY_MAX_GROUPS                                  */
+  int64_t rows, n, k;
+  int32_t a_type, b_type, c_type;   /* as gdy_gemm                                          */
+  int32_t trans_b;                  /* GDY_OVER_K: 0                                        */
+  const int32_t* offsets;           /* device                                               */
+  const void* a; int64_t lda;       /* device pointers; leading dimensions in elements      */
+  const void* b; int64_t ldb;
+  int64_t stride_b;                 /* GDY_OVER_ROWS: elements between the groups of B      */
+  void* c; int64_t ldc;
+  int64_t stride_c;                 /* GDY_OVER_K: elements between the groups of C         */
+  float scale_a, scale_b;           /* fp8 per-tensor scales; 1.0f for other types          */
+  const float* scales;              /* device, one fp32 scale a group (fp8 only), or NULL   */
+} gdy_grouped;
+
+/*
+ * Launch a grouped product on `hip_stream`, asynchronously.  `epilogue` may be NULL.
+ * Over rows it applies to the rows of C as to a GEMM's: residual and aux are rows x
+ * n, bias_grad is groups x n (stride_bias_grad 0: n sums over all groups) and bias
+ * groups x n (stride_bias 0: shared); stride_r and stride_aux are ignored.  Over K
+ * it may hold a residual only (R_e at stride_r; C itself accumulates into it).
+ * Aliasing rules as for gdy_execute_epilogue.  Allocates nothing; bias gradients use the
+ * context's split-K workspace (calls of one context must be ordered) and are refused
+ * (GDY_ERR_UNSUPPORTED) where a fp32 row of n for each tile of 16 to 256 rows does
+ * not fit into it.  Over K, A and B must end within 2 GiB; over rows only a group's B,
+ * and 512 rows of A and of C, have to.
+ */
+gdy_status gdy_execute_grouped(gdy_ctx* ctx, const gdy_grouped* product, const gdy_epilogue* epilogue,
+                               void* hip_stream);
+
+/*
+ * Activation and bias gradients that no product precedes:
+ *   dz(i,j) = round(dy(i,j) * f'(z(i,j)));  bias_grad_e(j) = the sum of dy * f'(z) over the rows of e,
+ * before its rounding, in fp32 and in an order that the sizes and offsets fix.  All
+ * matrices are rows x n of `type` (F16, BF16 or F32).  offsets as for gdy_grouped (rows
+ * of no group are left as they were), or NULL: one group of all rows.  dz may be
+ * dy or z itself (same pointer and leading dimension).
+ */
+typedef struct {
+  int64_t rows, n;
+  int32_t type;                     /* gdy_dtype                                            */
+  int32_t act;                      /* gdy_act; GDY_ACT_NONE: z is not read                 */
+  int32_t groups;                   /* with offsets: 0 .. GDY_MAX_GROUPS                    */
+  int32_t reserved;                 /* must be 0                                            */
+  const int32_t* offsets;           /* device, or NULL                                      */
+  const void* dy; int64_t lddy;
+  const void* z;  int64_t ldz;
+  void* dz;       int64_t lddz;     /* or NULL: bias_grad only                              */
+  float* bias_grad;                 /* groups x n (without offsets n), or NULL: dz only     */
+  int64_t stride_bias_grad;         /* elements between groups; 0: sums over all groups     */
+} gdy_act_grad;
+gdy_status gdy_execute_act_grad(gdy_ctx* ctx, const gdy_act_grad* op, void* hip_stream);
+
+/*
  * Per-kernel timing (Sec. 5.3 measures each GEMM's kernel runtime, with the
  * GEMMs run back-to-back on their streams).  When enabled, every dispatch
  * of gdy_execute records a start and a stop event on the stream it runs on

@@ -1,0 +1,117 @@
+// act_grad.h -- gradients around a linear layer that no product precedes: dz = dy *
+// f'(z) and the column sums of dz (over all rows, or over the rows of each group),
+// and the sums that finish every bias gradient of the library.
+//
+// Bound by memory: dy and z are read once and dz written once, 16 bytes a lane, the
+// sums stay in registers over a workgroup's rows.  Sums over many rows are
+// split: each workgroup writes one row of partial sums, bias_sums or group_sums
+// adds them in order (no atomics: the result does not depend on the run).
+#pragma once
+#include "grouped.h"
+
+namespace gdy {
+
+// 256 threads: 64 columns x 4 lanes of rows, added in order.
+__device__ __forceinline__ void column_sums(const float* part, float* out, int n, int rows, int col, float* lds) {
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
+  const bool live = col + lane < n;
+  float x = 0.0f;
+  if (live) {
+    const float* p = part + col + lane;
+#pragma unroll 8
+    for (int r = q; r < rows; r += 4) x += p[(int64_t)r * n];
+  }
+  lds[threadIdx.x] = x;
+  __syncthreads();
+  if (q == 0 && live) out[col + lane] = (lds[lane] + lds[64 + lane]) + (lds[128 + lane] + lds[192 + lane]);
+}
+
+static __global__ void __launch_bounds__(256) bias_sums(BiasSums s) {
+  __shared__ float lds[256];
+  int u = 0;
+  while (u + 1 < s.count && (int)blockIdx.x >= s.first[u + 1]) ++u;
+  const int blocks = (s.n[u] + 63) / 64, b = (int)blockIdx.x - s.first[u];
+  const int item = b / blocks;
+  column_sums(s.part[u] + (int64_t)item * s.rows[u] * s.n[u], s.out[u] + item * s.stride[u], s.n[u], s.rows[u],
+              (b - item * blocks) * 64, lds);
+}
+
+// The sums of group e, or of all groups (GroupSums::shared).
+static __global__ void __launch_bounds__(256) group_sums(GroupSums s) {
+  __shared__ float lds[256];
+  const int blocks = (s.n + 63) / 64, e = (int)blockIdx.x / blocks, col = ((int)blockIdx.x - e * blocks) * 64;
+  int first = 0, count;
+  if (s.shared) {
+    count = total_slots(s.offsets, s.groups, s.rows, s.bm, s.max_slots);
+  } else {
+    first = first_slot(s.offsets, s.groups, s.rows, s.bm, e);
+    const GroupRows g = group_rows(s.offsets, s.groups, s.rows, e);
+    count = min((g.count + s.bm - 1) / s.bm, max(s.max_slots - first, 0));
+  }
+  column_sums(s.part + (int64_t)first * s.n, s.out + e * s.stride, s.n, count, col, lds);
+}
+
+// A workgroup: bm rows of a group x kActCols columns, a lane eight consecutive ones.
+template <int DT>
+__global__ void __launch_bounds__(256) act_grad(KActGrad g) {
+  constexpr int OS = OutSize<DT>::v, LPR = kActCols / 8, RP = 256 / LPR, AHEAD = 4;
+  __shared__ __attribute__((aligned(16))) float lds[256 * 8];
+  const int tn = (g.n + kActCols - 1) / kActCols;
+  const int slot = (int)blockIdx.x / tn, n0 = ((int)blockIdx.x - slot * tn) * kActCols;
+  GroupSlot s = {0, 0, g.rows, 0};
+  if (g.offsets && !find_slot(g.offsets, g.groups, g.rows, g.bm, slot, s)) return;
+  const int r_lo = (slot - s.first) * g.bm;
+  const int m = uniform(min(g.bm, s.count - r_lo)), row = uniform(s.lo + r_lo);
+  const int cols = min(kActCols, g.n - n0);
+  // this tile of each matrix
+  auto tile = [&](const uint8_t* p, int ld) {
+    return make_rsrc(p ? p + ((int64_t)row * ld + n0) * OS : nullptr, p ? ((m - 1) * ld + cols) * OS : 0);
+  };
+  const Rsrc ry = tile(g.dy, g.lddy), rz = tile(g.z, g.ldz), rd = tile(g.dz, g.lddz);
+  const int tid = threadIdx.x, c8 = (tid % LPR) * 8, left = cols - c8;
+  const bool y_vec = OS == 4 || g.dy_vec, z_vec = OS == 4 || g.z_vec, d_vec = OS == 4 || g.dz_vec;
+  float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  if (left > 0) {
+    for (int r0 = tid / LPR; r0 < m; r0 += RP * AHEAD) {
+      Row8<DT> y[AHEAD], z[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int r = r0 + u * RP;
+        if (r >= m) break;
+        y[u].load(ry, (r * g.lddy + c8) * OS, y_vec, left);
+        if (g.z) z[u].load(rz, (r * g.ldz + c8) * OS, z_vec, left);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int r = r0 + u * RP;
+        if (r >= m) break;
+        float x[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = y[u].get(q);
+        if (g.z) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) x[q] *= act_slope(z[u].get(q), g.act);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum[q] += x[q];
+        if (g.dz) {
+          Row8<DT> w;
+          w.set(x);
+          w.store(rd, (r * g.lddz + c8) * OS, d_vec, left);
+        }
+      }
+    }
+  }
+  if (!g.part) return;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) lds[(tid / LPR) * kActCols + c8 + q] = sum[q];
+  __syncthreads();
+  for (int c = tid; c < cols; c += 256) {
+    float x = lds[c];
+#pragma unroll
+    for (int r = 1; r < RP; ++r) x += lds[r * kActCols + c];
+    g.part[(int64_t)slot * g.n + n0 + c] = x;
+  }
+}
+
+}  // namespace gdy

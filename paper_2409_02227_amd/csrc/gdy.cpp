@@ -1534,6 +1534,80 @@ void build_reduce(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, co
   (void)p;
 }
 
+// Whether an epilogue changes anything.
+bool has_epilogue(const gdy_epilogue& e) {
+  return e.act != GDY_ACT_NONE || e.bias || e.residual || e.aux || e.bias_grad;
+}
+
+// The epilogue kernels of an input type (gdy_internal.h: ep_*).
+const void* epilogue_kernel(int dtype, int family) {
+  return dtype == DT_BF16 ? ep_bf16(family) : dtype == DT_F16 ? ep_f16(family)
+         : dtype == DT_FP8 ? ep_fp8(family) : dtype == DT_F32 ? ep_f32(family) : nullptr;
+}
+
+// Rows of partial column sums that an item of g may take: its tile rows, or those
+// of the split reduction.  Members of 256 x 256 kernels may run 128-row tiles.
+int64_t part_rows(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
+  if (p.split_of[i] > 1) return (g.m + kEpiReduceRows - 1) / kEpiReduceRows;
+  const int bm = std::min(exec_of(ctx, p.variant_of[i], g).jbm, 128);
+  return (g.m + bm - 1) / bm;
+}
+int64_t part_bytes(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
+  return (part_rows(ctx, g, p, i) * g.n * std::max(g.batch, 1) * 4 + 255) / 256 * 256;
+}
+
+// Where the partial column sums of a submission's bias gradients lie in the
+// workspace (-1: none): behind the split planes of their group.  need: bytes of
+// the workspace in use at once.
+std::vector<int64_t> part_offsets(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue* ep, const gdy_plan_t& p,
+                                  int mode, const std::vector<int64_t>& ws_off, int64_t* need) {
+  std::vector<int64_t> off(std::max(p.n, 1), -1);
+  *need = 0;
+  for (int t = 0, end = 0; t < GDY_MAX_GEMMS && p.order[t] >= 0; t = end) {
+    const int grp = p.group_of[p.order[t]];
+    int64_t ws = 0;
+    for (end = t; end < GDY_MAX_GEMMS && p.order[end] >= 0 && p.group_of[p.order[end]] == grp; ++end)
+      if (ws_off[p.order[end]] >= 0)
+        ws = std::max(ws, ws_off[p.order[end]] + split_ws_bytes(g[p.order[end]], p.split_of[p.order[end]]));
+    for (int u = t; u < end; ++u) {
+      const int i = p.order[u];
+      if (!ep[i].bias_grad) continue;
+      off[i] = ws;
+      if (mode != GDY_SEQUENTIAL) ws += part_bytes(ctx, g[i], p, i);
+      *need = std::max(*need, off[i] + part_bytes(ctx, g[i], p, i));
+    }
+    *need = std::max(*need, ws);
+  }
+  return off;
+}
+
+// The epilogue of a launch's member u, whose KArgs are built.
+KEpi make_epi(const gdy_gemm& g, const gdy_epilogue& e, const KArgs& a, float* part) {
+  KEpi k;
+  std::memset(&k, 0, sizeof k);
+  const int os = out_size(g);
+  const bool batched = g.batch > 1;
+  auto vec = [&](const void* ptr, int64_t ld, int64_t stride) {
+    return (uintptr_t)ptr % 8 == 0 && (ld * os) % 8 == 0 && (!batched || (stride * os) % 8 == 0);
+  };
+  k.bias = (const uint8_t*)e.bias;
+  k.bias_f32 = e.bias && e.bias_type == GDY_F32;
+  k.stride_bias = batched ? e.stride_bias * (k.bias_f32 ? 4 : os) : 0;
+  k.res = (const uint8_t*)e.residual;
+  k.ldr = (int32_t)e.ldr;
+  k.stride_res = batched ? e.stride_r * os : 0;
+  k.res_vec = vec(e.residual, e.ldr, e.stride_r);
+  k.aux = e.grad && e.act == GDY_ACT_NONE ? nullptr : (uint8_t*)e.aux;
+  k.ldaux = (int32_t)e.ldaux;
+  k.stride_aux = batched ? e.stride_aux * os : 0;
+  k.aux_vec = vec(e.aux, e.ldaux, e.stride_aux);
+  k.act = e.act;
+  k.grad = e.grad;
+  k.part = part;
+  k.part_rows = a.split > 1 ? (int32_t)((g.m + kEpiReduceRows - 1) / kEpiReduceRows) : a.tiles_m;
+  return k;
+}
+
 // Split-K workspace offsets per GEMM (-1: unsplit): consecutive regions per
 // group in launch order (the groups run one after another and reuse the
 // workspace; in SEQUENTIAL each GEMM runs alone on the origin stream and
@@ -1763,8 +1837,67 @@ void plan_units(const gdy_ctx* ctx, const gdy_gemm* g, gdy_plan_t* p, int mode, 
   }
 }
 
-gdy_status launch_plan(gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int mode,
-                       const Launches& launches, hipStream_t origin, float* ws_base, int64_t ws_cap) {
+void add_bias_sum(BiasSums* s, const float* part, float* out, int n, int rows, int items, int64_t stride);
+hipError_t launch_bias_sums(BiasSums* s, hipStream_t hs, hipEvent_t stop);
+
+// The epilogue launch of a unit: its members on the epilogue kernel of their
+// family, the reduction of the split ones, and the sums of the bias gradients.
+gdy_status launch_epilogues(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue* ep, const Members& members,
+                            int family, int dtype, const KLaunch& launch, int grid, bool split, float* ws_base,
+                            const std::vector<int64_t>& part_off, hipStream_t hs, hipEvent_t start, hipEvent_t stop) {
+  KEpis epis;
+  BiasSums sums;
+  sums.count = 0;
+  bool any_sums = false;
+  for (int u = 0; u < launch.count; ++u) {
+    const int i = members[u];
+    epis.e[u] = make_epi(g[i], ep[i], launch.g[u], part_off[i] >= 0 ? ws_base + part_off[i] / 4 : nullptr);
+    any_sums = any_sums || ep[i].bias_grad;
+  }
+  void* argv[] = {(void*)&launch, &epis};
+  hipError_t e = hipExtLaunchKernel(epilogue_kernel(dtype, family), dim3(grid), dim3(family == 1 ? 256 : 512), argv, 0,
+                                    hs, start, !split && !any_sums ? stop : nullptr, 0);
+  if (e == hipSuccess && split) {
+    KLaunch red;
+    KEpis repis;
+    std::memset(&red, 0, sizeof red);
+    int64_t wg = 0;
+    for (int u = 0; u < launch.count; ++u) {
+      if (launch.g[u].split <= 1) continue;
+      const gdy_gemm& x = g[members[u]];
+      const int c = red.count++;
+      red.g[c] = launch.g[u];
+      repis.e[c] = epis.e[u];
+      red.first[c] = (int32_t)wg;
+      wg += (x.m + kEpiReduceRows - 1) / kEpiReduceRows * ((x.n + 127) / 128) * std::max<int64_t>(x.batch, 1);
+    }
+    red.first[red.count] = (int32_t)wg;
+    void* rargv[] = {&red, &repis};
+    e = hipExtLaunchKernel(epilogue_kernel(dtype, 0), dim3((unsigned)wg), dim3(256), rargv, 0, hs, nullptr,
+                           !any_sums ? stop : nullptr, 0);
+  }
+  if (e == hipSuccess && any_sums) {
+    for (int u = 0; u < launch.count; ++u) {
+      const int i = members[u];
+      if (!ep[i].bias_grad) continue;
+      const int items = std::max(g[i].batch, 1);
+      const bool shared = items > 1 && ep[i].stride_bias_grad == 0;
+      add_bias_sum(&sums, epis.e[u].part, ep[i].bias_grad, (int)g[i].n,
+                   shared ? epis.e[u].part_rows * items : epis.e[u].part_rows, shared ? 1 : items,
+                   ep[i].stride_bias_grad);
+    }
+    e = launch_bias_sums(&sums, hs, stop);
+  }
+  if (e != hipSuccess)
+    return fail(ctx, GDY_ERR_HIP, "launch with epilogues (%d GEMMs, first %d) failed: %s", members.size(), members[0],
+                hipGetErrorString(e));
+  return GDY_OK;
+}
+
+// ep: the members' epilogues, or null; part_off: as part_offsets gives them.
+gdy_status launch_plan(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue* ep, const gdy_plan_t& p, int mode,
+                       const Launches& launches, hipStream_t origin, float* ws_base, int64_t ws_cap,
+                       const std::vector<int64_t>& part_off) {
   gdy_status st = GDY_OK;
   const int n = p.n;
   // stream slots: the pool (or the active CU budget's pool), or the CU
@@ -1822,10 +1955,26 @@ gdy_status launch_plan(gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int
       KLaunch launch;
       int grid = 0;
       bool split = false;
-      st = build_launch(ctx, g, p, mode, members, x.joint, ws_off, ws_base, ws_cap, &launch, &grid, &split);
+      // members with epilogues run on the epilogue kernel of their family, in the
+      // family's tiles
+      bool with_ep = false;
+      for (int i : members) with_ep = with_ep || (ep && has_epilogue(ep[i]));
+      const int joint = with_ep && !x.joint ? ex.family : x.joint;
+      st = build_launch(ctx, g, p, mode, members, joint, ws_off, ws_base, ws_cap, &launch, &grid, &split);
       if (st != GDY_OK) break;
       void* argv[] = {&launch};
       const int d = x.dispatch;
+      if (with_ep) {
+        st = launch_epilogues(ctx, g, ep, members, joint, g[i0].a_type, launch, grid, split, ws_base, part_off,
+                              p.stream_of[i0] >= 0 ? stream_at(p.stream_of[i0]) : origin, ts ? ts->start[d] : nullptr,
+                              ts ? ts->stop[d] : nullptr);
+        if (st != GDY_OK) break;
+        if (ts) {
+          ts->launched[d] = 1;
+          for (int i : members) ts->dispatch_of[i] = d;
+        }
+        continue;
+      }
       const void* func = x.joint ? joint_kernel(g[i0].a_type, x.joint) : split ? ex.func_split : ex.func;
       const int waves = !x.joint ? ex.waves : x.joint == 1 ? 4 : 8;
       hipStream_t hs = p.stream_of[i0] >= 0 ? stream_at(p.stream_of[i0]) : origin;
@@ -2034,6 +2183,8 @@ gdy_status load_table(gdy_ctx* ctx, const char* path) {
 // ---------------------------------------------------------------------------
 // C-ABI
 // ---------------------------------------------------------------------------
+#include "operators.h"
+
 extern "C" {
 
 const char* gdy_status_string(gdy_status s) {
@@ -2322,12 +2473,13 @@ gdy_status gdy_set_rc(gdy_ctx* ctx, int32_t budget_cus) {
   return fail(ctx, GDY_ERR_INVALID_ARG, "no CU-masked pool for %d CUs", budget_cus);
 }
 
-static gdy_status plan_impl(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, int32_t mode, int32_t forced_cd,
-                            gdy_plan_t* out, Launches* launches) {
+static gdy_status plan_impl(gdy_ctx* ctx, const gdy_gemm* gemms, const gdy_epilogue* ep, int32_t n, int32_t mode,
+                            int32_t forced_cd, gdy_plan_t* out, Launches* launches) {
   if (!ctx || !out) return GDY_ERR_INVALID_ARG;
   ctx->err.clear();
   try {
     gdy_status s = validate(ctx, gemms, n, mode);
+    if (s == GDY_OK && ep) s = validate_epilogues(ctx, gemms, ep, n);
     if (s != GDY_OK) return s;
     if (partition_mode(mode) && forced_cd != 0 && forced_cd != 2 && forced_cd != 4 && forced_cd != 8)
       return fail(ctx, GDY_ERR_INVALID_ARG, "CU-Partition takes 2, 4 or 8 partitions, not %d", forced_cd);
@@ -2344,33 +2496,53 @@ static gdy_status plan_impl(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, int3
 gdy_status gdy_plan(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, int32_t mode, int32_t forced_cd,
                     gdy_plan_t* out) {
   Launches launches;
-  return plan_impl(ctx, gemms, n, mode, forced_cd, out, &launches);
+  return plan_impl(ctx, gemms, nullptr, n, mode, forced_cd, out, &launches);
 }
 
-static gdy_status execute_impl(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, int32_t mode, int32_t forced_cd,
-                               void* hip_stream, gdy_plan_t* out, bool use_static) {
+// The context's device for the length of a call.
+struct DeviceGuard {
+  int before = -1;
+  hipError_t enter(int device) {
+    if (hipGetDevice(&before) == hipSuccess && before == device) {
+      before = -1;
+      return hipSuccess;
+    }
+    return hipSetDevice(device);
+  }
+  ~DeviceGuard() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+static gdy_status execute_impl(gdy_ctx* ctx, const gdy_gemm* gemms, const gdy_epilogue* ep, int32_t n, int32_t mode,
+                               int32_t forced_cd, void* hip_stream, gdy_plan_t* out, bool use_static) {
   if (!ctx) return GDY_ERR_INVALID_ARG;
   gdy_plan_t local;
   gdy_plan_t* p = out ? out : &local;
   Launches launches;
-  gdy_status s = plan_impl(ctx, gemms, n, mode, forced_cd, p, &launches);
+  gdy_status s = plan_impl(ctx, gemms, ep, n, mode, forced_cd, p, &launches);
   if (s != GDY_OK) return s;
   if (ctx->device < 0) return fail(ctx, GDY_ERR_UNSUPPORTED, "host-only context cannot execute");
-  float* ws = ctx->split_ws;
-  int64_t cap = kSplitWsBytes;
-  if (use_static) {
-    const int64_t need = plan_ws_need(gemms, *p, mode);
-    if (need > (int64_t)GDY_STATIC_SCRATCH_BYTES)
-      return fail(ctx, GDY_ERR_UNSUPPORTED,
-                  "the plan needs %lld bytes of split-K scratch at once; the static array holds %lld",
-                  (long long)need, (long long)GDY_STATIC_SCRATCH_BYTES);
-    ws = ctx->scratch;
-    cap = GDY_STATIC_SCRATCH_BYTES;
-  }
-  int cur = -1;
-  if (hipGetDevice(&cur) != hipSuccess || cur != ctx->device) HIP_TRY(ctx, hipSetDevice(ctx->device));
   try {
-    return launch_plan(ctx, gemms, *p, mode, launches, (hipStream_t)hip_stream, ws, cap);
+    float* ws = use_static ? ctx->scratch : ctx->split_ws;
+    const int64_t cap = use_static ? (int64_t)GDY_STATIC_SCRATCH_BYTES : kSplitWsBytes;
+    int64_t need = use_static ? plan_ws_need(gemms, *p, mode) : 0;
+    std::vector<int64_t> part_off;
+    if (ep) {
+      int64_t parts = 0;
+      part_off = part_offsets(ctx, gemms, ep, *p, mode, ws_offsets(gemms, *p, mode), &parts);
+      need = std::max(need, parts);
+    }
+    if (need > cap)
+      return fail(ctx, GDY_ERR_UNSUPPORTED,
+                  use_static ? "the plan needs %lld bytes of split-K scratch at once; the static array holds %lld"
+                             : "the plan needs %lld bytes of workspace at once; the context's holds %lld",
+                  (long long)need, (long long)cap);
+    DeviceGuard guard;
+    HIP_TRY(ctx, guard.enter(ctx->device));
+    s = launch_plan(ctx, gemms, ep, *p, mode, launches, (hipStream_t)hip_stream, ws, cap, part_off);
+    if (s == GDY_OK && ep) s = zero_bias_grads(ctx, gemms, ep, n, (hipStream_t)hip_stream);
+    return s;
   } catch (...) {
     return fail(ctx, GDY_ERR_NOMEM, "host allocation failed");
   }
@@ -2378,12 +2550,55 @@ static gdy_status execute_impl(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, i
 
 gdy_status gdy_execute(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, int32_t mode, int32_t forced_cd,
                        void* hip_stream, gdy_plan_t* out) {
-  return execute_impl(ctx, gemms, n, mode, forced_cd, hip_stream, out, false);
+  return execute_impl(ctx, gemms, nullptr, n, mode, forced_cd, hip_stream, out, false);
 }
 
 gdy_status gdy_execute_static(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, int32_t mode, int32_t forced_cd,
                               void* hip_stream, gdy_plan_t* out) {
-  return execute_impl(ctx, gemms, n, mode, forced_cd, hip_stream, out, true);
+  return execute_impl(ctx, gemms, nullptr, n, mode, forced_cd, hip_stream, out, true);
+}
+
+gdy_status gdy_execute_epilogue(gdy_ctx* ctx, const gdy_gemm* gemms, const gdy_epilogue* epilogues, int32_t n,
+                                int32_t mode, int32_t forced_cd, void* hip_stream, gdy_plan_t* out) {
+  return execute_impl(ctx, gemms, epilogues, n, mode, forced_cd, hip_stream, out, false);
+}
+
+gdy_status gdy_execute_epilogue_static(gdy_ctx* ctx, const gdy_gemm* gemms, const gdy_epilogue* epilogues, int32_t n,
+                                       int32_t mode, int32_t forced_cd, void* hip_stream, gdy_plan_t* out) {
+  return execute_impl(ctx, gemms, epilogues, n, mode, forced_cd, hip_stream, out, true);
+}
+
+gdy_status gdy_execute_grouped(gdy_ctx* ctx, const gdy_grouped* product, const gdy_epilogue* epilogue,
+                               void* hip_stream) {
+  if (!ctx) return GDY_ERR_INVALID_ARG;
+  ctx->err.clear();
+  try {
+    if (!product) return fail(ctx, GDY_ERR_INVALID_ARG, "null product");
+    const gdy_status s = validate_grouped(ctx, *product, epilogue);
+    if (s != GDY_OK) return s;
+    if (ctx->device < 0) return fail(ctx, GDY_ERR_UNSUPPORTED, "host-only context cannot execute");
+    DeviceGuard guard;
+    HIP_TRY(ctx, guard.enter(ctx->device));
+    return launch_grouped(ctx, *product, epilogue, (hipStream_t)hip_stream);
+  } catch (...) {
+    return fail(ctx, GDY_ERR_NOMEM, "host allocation failed");
+  }
+}
+
+gdy_status gdy_execute_act_grad(gdy_ctx* ctx, const gdy_act_grad* op, void* hip_stream) {
+  if (!ctx) return GDY_ERR_INVALID_ARG;
+  ctx->err.clear();
+  try {
+    if (!op) return fail(ctx, GDY_ERR_INVALID_ARG, "null operator");
+    const gdy_status s = validate_act_grad(ctx, *op);
+    if (s != GDY_OK) return s;
+    if (ctx->device < 0) return fail(ctx, GDY_ERR_UNSUPPORTED, "host-only context cannot execute");
+    DeviceGuard guard;
+    HIP_TRY(ctx, guard.enter(ctx->device));
+    return launch_act_grad(ctx, *op, (hipStream_t)hip_stream);
+  } catch (...) {
+    return fail(ctx, GDY_ERR_NOMEM, "host allocation failed");
+  }
 }
 
 gdy_status gdy_dispatch_map(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, int32_t mode, int32_t forced_cd,
@@ -2393,7 +2608,7 @@ gdy_status gdy_dispatch_map(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, int3
     return GDY_ERR_INVALID_ARG;
   gdy_plan_t p;
   Launches launches;
-  gdy_status s = plan_impl(ctx, gemms, n, mode, forced_cd, &p, &launches);
+  gdy_status s = plan_impl(ctx, gemms, nullptr, n, mode, forced_cd, &p, &launches);
   if (s != GDY_OK) return s;
   if (dispatch < 0 || dispatch >= p.n_dispatches) return fail(ctx, GDY_ERR_INVALID_ARG, "no dispatch %d", dispatch);
   try {

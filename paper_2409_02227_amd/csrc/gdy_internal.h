@@ -108,6 +108,87 @@ __host__ __device__ inline void locate(const KLaunch& L, int b, int& gi, int& lw
   nwg = L.first[gi + 1] - L.first[gi];
 }
 
+// Activations, numerically equal to the public gdy_act values.
+enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU = 4 };
+
+// The epilogue of one member.  Strides are bytes between items of a batch.
+struct KEpi {
+  const uint8_t* bias;   // N values (null: none)
+  const uint8_t* res;    // M x N of C's type (null: none); may be C itself
+  uint8_t* aux;          // M x N of C's type: written (grad: read)
+  float* part;           // column sums of C by tile row: part_rows rows of N per item (null: none)
+  int64_t stride_bias, stride_res, stride_aux;
+  int32_t ldr, ldaux;    // elements
+  int32_t part_rows;
+  int32_t bias_f32;      // 1: bias is fp32, else of C's type
+  int32_t act, grad;
+  int32_t res_vec, aux_vec;  // 1: rows allow 16-byte accesses (KArgs::c_vec's rule)
+};
+struct KEpis {
+  KEpi e[kMaxFused];
+};
+
+// The split reduction with epilogues takes this many rows a tile.
+constexpr int kEpiReduceRows = 16;
+
+// A product grouped by expert (grouped.h).
+struct KGroup {
+  const uint8_t* a;
+  const uint8_t* b;
+  uint8_t* c;
+  const int32_t* offsets;  // groups + 1
+  const float* scales;     // one per group (null: 1)
+  int64_t stride_b;        // bytes between groups of B
+  int64_t stride_c;        // over K: bytes between groups of C
+  int32_t rows, groups;
+  int32_t m, n, k;         // over rows: C is rows x n, K = k; over K: C_e is m x n
+  int32_t lda, ldb, ldc;   // elements
+  float scale;
+  int32_t a_dma, b_dma, c_vec;
+  int32_t max_slots;       // over rows: the most row tiles
+  KEpi epi;                // over K: the residual only; strides between groups
+};
+
+// A kernel of grouped products: its tile and threads.  Tiles by index: 256 x 256,
+// 128 x 128, 64 x 128 (over K 64 x 64), and over rows 32 x 128 and 16 x 64.
+struct GroupKernel {
+  const void* func;
+  int bm, bn, threads;
+};
+
+// Partial sums to a bias gradient: out[item][j] = sum over `rows` rows of part.
+struct BiasSums {
+  int32_t count;
+  int32_t first[kMaxFused + 1];  // workgroup ranges: 64 columns of an item each
+  const float* part[kMaxFused];
+  float* out[kMaxFused];
+  int64_t stride[kMaxFused];     // between items of out
+  int32_t n[kMaxFused], rows[kMaxFused];
+};
+
+// The partial sums of grouped rows: those of group e's row tiles of bm rows, to
+// out[e]; shared: of all groups, to out[0].
+struct GroupSums {
+  const float* part;
+  float* out;
+  const int32_t* offsets;
+  int64_t stride;
+  int32_t n, rows, groups, bm, max_slots, shared;
+};
+// dz = dy * f'(z), and partial column sums by row tile.
+struct KActGrad {
+  const uint8_t* dy;
+  const uint8_t* z;        // null where f is the identity
+  uint8_t* dz;             // null: not written
+  const int32_t* offsets;  // null: one group of all rows
+  float* part;             // row tiles x n (null: no sums)
+  int32_t rows, groups, n, bm, max_slots;
+  int32_t lddy, ldz, lddz, act;
+  int32_t dy_vec, z_vec, dz_vec;
+};
+
+constexpr int kActCols = 512;  // columns of a workgroup
+
 // Compile-time description of one instantiated kernel.
 struct KernelDesc {
   const char* name;   // e.g. "bf16_nn_256x256_w8_m32"
@@ -141,6 +222,19 @@ const void* joint_bf16(int family);
 const void* joint_f16(int family);
 const void* joint_fp8(int family);
 const void* joint_f32(int family);
+// Kernels of launches with epilogues: of a family (1, 2), or the split-K
+// reduction (0); null if there is none.
+const void* ep_bf16(int family);
+const void* ep_f16(int family);
+const void* ep_fp8(int family);
+const void* ep_f32(int family);
+GroupKernel group_bf16(int over_k, int tb, int tile);
+GroupKernel group_f16(int over_k, int tb, int tile);
+GroupKernel group_fp8(int over_k, int tb, int tile);
+GroupKernel group_f32(int over_k, int tb, int tile);
+const void* act_grad_kernel(int dt);  // null: no such type
+const void* bias_sum_kernel();
+const void* group_sum_kernel();
 int kernels_d_bf16(const KernelDesc** out);
 int kernels_d_f16(const KernelDesc** out);
 int kernels_d_fp8(const KernelDesc** out);

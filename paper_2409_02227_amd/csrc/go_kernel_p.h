@@ -48,7 +48,7 @@
 // (six), after that.
 // Copies past the last K tile read nothing (out of range) and keep the count.
 #pragma once
-#include "lds_copy.h"
+#include "epilogue.h"
 
 namespace gdy {
 
@@ -106,9 +106,9 @@ template <int ES, bool KC, bool SPILLS> struct PhaseCopy {
 };
 
 // The tiles of one member (work items lwg, lwg + nwg, ... of p), in the kPLds
-// bytes at smem.
-template <int DT, int TA, int TB, bool JOINT>
-__device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds_u8* smem) {
+// bytes at smem.  EP: where the results go (NoEpi: to C, scaled and rounded).
+template <int DT, int TA, int TB, bool JOINT, class EP = NoEpi>
+__device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds_u8* smem, EP ep = EP()) {
   const Args<JOINT> own(args);
   const KArgs& p = own.v;
   if constexpr (JOINT) lwg = uniform(lwg), nwg = uniform(nwg);
@@ -279,6 +279,37 @@ __device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds
     // two rows an instruction, where the accumulators' own order gives 32.
     // The 528-byte row pitch keeps a half wave's 16 rows of 16 bytes on
     // distinct banks.
+    if constexpr (EP::on) {  // fp32 rows, a half of the tile at a time (133 of the 144 KiB)
+      typedef EpiTile<DT, 256, 512> Epi;
+      static_assert(128 * Epi::PITCH <= kPLds, "half of the tile fits in the ring");
+      Epi x(ep(item, tm), n0, (int)threadIdx.x);
+      auto dump = [&](const Acc (&h)[2][2][4]) {
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              *(__attribute__((address_space(3))) f32x4*)(smem + (wm * 64 + i * 16 + (lane & 15)) * Epi::PITCH +
+                                                          (hb * 128 + wn * 32 + j * 16 + 4 * (lane >> 4)) * 4) =
+                  h[hb][j][i];
+      };
+#pragma unroll 1
+      for (int ha = 0; ha < (half ? 1 : 2); ++ha) {
+        if (ha == 0) {
+          dump(acc[0]);
+        } else {
+          __syncthreads();  // the first half has been read
+          dump(acc[1]);
+        }
+        __syncthreads();
+        x.rows(smem, m0 + ha * 128, min(128, Mrows - m0 - ha * 128));
+      }
+      if (x.o.part) {
+        __syncthreads();
+        x.sums(smem);
+      }
+    } else {
     const float s = p.scale;
 #pragma unroll
     for (int ha = 0; ha < 2; ++ha) {
@@ -299,6 +330,7 @@ __device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds
     __syncthreads();
     store_tile<256, 512, kPOutRow>(smem, rc, m0 * ldc_b + n0 * 2, ldc_b, min(half ? 128 : 256, Mrows - m0),
                                    min(256, Ncols - n0), p.c_vec != 0, (int)threadIdx.x);
+    }
     if (tb + nwg < total) __syncthreads();  // the next tile's copies overwrite the output rows
   }
 }

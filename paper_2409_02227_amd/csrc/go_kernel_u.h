@@ -141,9 +141,11 @@ template <int DT, int BM, int BN, int WM, int WN, int STAGES> struct UCfg {
 
 // The tiles of one member: work items lwg, lwg + nwg, ... of p, by the whole
 // workgroup, in the LDS at smem (UCfg::LDS bytes).  ANY: both ways, else
-// copies only.  SPLIT: members may be split along K.
-template <int DT, int TA, int TB, int BM, int BN, int WM, int WN, int STAGES, bool ANY, bool SPLIT, bool JOINT>
-__device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds_u8* smem) {
+// copies only.  SPLIT: members may be split along K.  EP: where the results
+// go (NoEpi: to C, scaled and rounded).
+template <int DT, int TA, int TB, int BM, int BN, int WM, int WN, int STAGES, bool ANY, bool SPLIT, bool JOINT,
+          class EP = NoEpi>
+__device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds_u8* smem, EP ep = EP()) {
   const Args<JOINT> own(args);
   const KArgs& p = own.v;
   if constexpr (JOINT) lwg = uniform(lwg), nwg = uniform(nwg);
@@ -411,6 +413,31 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
 
     // accumulator r of lane l is n = 4*(l/16) + r, m = l%16 of its block
     __syncthreads();  // every wave has read its last fragments
+    if constexpr (EP::on) {  // fp32 rows, up to 64 at a time
+      typedef EpiTile<DT, BN, C::NW * 64> Epi;
+      constexpr int HR = BM < 64 ? BM : 64;
+      static_assert(HR * Epi::PITCH <= C::LDS && C::NW * 64 * 32 <= C::LDS, "the rows and the sums fit in the ring");
+      Epi x(ep(item, tm), n0, tid);
+#pragma unroll 1
+      for (int h = 0; h < BM / HR && m0 + h * HR < Mrows; ++h) {
+        if (h) __syncthreads();  // the rows before have been read
+#pragma unroll
+        for (int i = 0; i < C::FM; ++i) {
+          const int r = wm * WTM + i * 16 - h * HR;
+          if (r < 0 || r >= HR) continue;
+#pragma unroll
+          for (int j = 0; j < C::FN; ++j)
+            *(__attribute__((address_space(3))) f32x4*)(smem + (r + (lane & 15)) * Epi::PITCH +
+                                                        (wn * WTN + j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i];
+        }
+        __syncthreads();
+        x.rows(smem, m0 + h * HR, min(HR, Mrows - m0 - h * HR));
+      }
+      if (x.o.part) {
+        __syncthreads();
+        x.sums(smem);
+      }
+    } else {
     const float s = p.scale;
     if constexpr (C::ES == 4) {  // 16 bytes a lane, 64 consecutive ones of 16 rows an instruction
 #pragma unroll
@@ -443,6 +470,7 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
     __syncthreads();
     store_tile<BN, C::NW * 64, C::PITCH>(smem, rc, m0 * ldc_b + n0 * 2, ldc_b, min(BM, Mrows - m0),
                                          min(BN, Ncols - n0), p.c_vec != 0, tid);
+    }
     }
     if (tb + nwg < total) __syncthreads();  // the next tile's copies overwrite the output rows
   }
@@ -480,16 +508,16 @@ constexpr int kJointBm[5] = {128, 64, 64, 32, 16}, kJointBn[5] = {128, 128, 64, 
 constexpr int joint_code(int ta, int tb, int bm, int bn) { return (2 * ta + tb) * 8 + joint_tile(bm, bn); }
 constexpr int kJointLds = 80 * 1024;
 
-template <int DT, int TA, int TB>
-__device__ __forceinline__ void joint_tiles(const KArgs& p, int lwg, int nwg, lds_u8* smem) {
+template <int DT, int TA, int TB, class EP = NoEpi>
+__device__ __forceinline__ void joint_tiles(const KArgs& p, int lwg, int nwg, lds_u8* smem, EP ep = EP()) {
   switch (p.code & 7) {
-    case 0: u_tiles<DT, TA, TB, 128, 128, 2, 2, 2, true, true, true>(p, lwg, nwg, smem); break;
-    case 2: u_tiles<DT, TA, TB, 64, 64, 2, 2, 4, true, true, true>(p, lwg, nwg, smem); break;
-    case 4: u_tiles<DT, TA, TB, 16, 64, 1, 4, 2, true, true, true>(p, lwg, nwg, smem); break;
+    case 0: u_tiles<DT, TA, TB, 128, 128, 2, 2, 2, true, true, true, EP>(p, lwg, nwg, smem, ep); break;
+    case 2: u_tiles<DT, TA, TB, 64, 64, 2, 2, 4, true, true, true, EP>(p, lwg, nwg, smem, ep); break;
+    case 4: u_tiles<DT, TA, TB, 16, 64, 1, 4, 2, true, true, true, EP>(p, lwg, nwg, smem, ep); break;
     default:  // the catalogue has these for an untransposed A only
       if constexpr (TA == 0) {
-        if ((p.code & 7) == 1) u_tiles<DT, TA, TB, 64, 128, 2, 2, 3, true, true, true>(p, lwg, nwg, smem);
-        else u_tiles<DT, TA, TB, 32, 128, 1, 4, 4, true, true, true>(p, lwg, nwg, smem);
+        if ((p.code & 7) == 1) u_tiles<DT, TA, TB, 64, 128, 2, 2, 3, true, true, true, EP>(p, lwg, nwg, smem, ep);
+        else u_tiles<DT, TA, TB, 32, 128, 1, 4, 4, true, true, true, EP>(p, lwg, nwg, smem, ep);
       }
   }
 }

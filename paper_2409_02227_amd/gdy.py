@@ -25,6 +25,10 @@ F16, BF16, FP8_E4M3, F32 = 1, 2, 3, 4
 SEQUENTIAL, DEFAULT, GO, SELECTOR, FORCED, FORCED_GROUPED = 0, 1, 2, 3, 4, 5
 CU_PARTITION, CU_PARTITION_GO, CU_PARTITION_RC = 6, 7, 8
 GEMM, ADD = 0, 1  # gdy_op
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4  # gdy_act
+ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
+OVER_ROWS, OVER_K = 0, 1  # gdy_over
+MAX_GROUPS = 4096
 MODES = {"sequential": SEQUENTIAL, "default": DEFAULT, "go": GO,
          "selector": SELECTOR, "forced": FORCED, "forced_grouped": FORCED_GROUPED,
          "cu_partition": CU_PARTITION, "cu_partition_go": CU_PARTITION_GO,
@@ -36,6 +40,7 @@ STATUS = {0: "GDY_OK", 1: "GDY_ERR_INVALID_ARG", 2: "GDY_ERR_UNSUPPORTED", 3: "G
           4: "GDY_ERR_TOO_MANY", 5: "GDY_ERR_TABLE", 6: "GDY_ERR_HIP", 7: "GDY_ERR_NOMEM"}
 
 EXPORTS = ("gdy_create", "gdy_destroy", "gdy_set_rc", "gdy_plan", "gdy_execute", "gdy_execute_static",
+           "gdy_execute_epilogue", "gdy_execute_epilogue_static", "gdy_execute_grouped", "gdy_execute_act_grad",
            "gdy_set_timing", "gdy_last_kernel_times", "gdy_kernel_times", "gdy_features", "gdy_dispatch_map",
            "gdy_variant_count",
            "gdy_variant_info", "gdy_variant_find", "gdy_isolated_variant",
@@ -54,6 +59,35 @@ class GemmDesc(ctypes.Structure):
                 ("batch", ctypes.c_int32), ("op", ctypes.c_int32),
                 ("stride_a", ctypes.c_int64), ("stride_b", ctypes.c_int64),
                 ("stride_c", ctypes.c_int64)]
+
+
+class EpilogueDesc(ctypes.Structure):
+    _fields_ = [("act", ctypes.c_int32), ("grad", ctypes.c_int32),
+                ("bias", ctypes.c_void_p), ("bias_type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("aux", ctypes.c_void_p), ("ldaux", ctypes.c_int64),
+                ("bias_grad", ctypes.c_void_p),
+                ("stride_bias", ctypes.c_int64), ("stride_r", ctypes.c_int64),
+                ("stride_aux", ctypes.c_int64), ("stride_bias_grad", ctypes.c_int64)]
+
+
+class GroupedDesc(ctypes.Structure):
+    _fields_ = [("over", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64),
+                ("a_type", ctypes.c_int32), ("b_type", ctypes.c_int32), ("c_type", ctypes.c_int32),
+                ("trans_b", ctypes.c_int32), ("offsets", ctypes.c_void_p),
+                ("a", ctypes.c_void_p), ("lda", ctypes.c_int64),
+                ("b", ctypes.c_void_p), ("ldb", ctypes.c_int64), ("stride_b", ctypes.c_int64),
+                ("c", ctypes.c_void_p), ("ldc", ctypes.c_int64), ("stride_c", ctypes.c_int64),
+                ("scale_a", ctypes.c_float), ("scale_b", ctypes.c_float), ("scales", ctypes.c_void_p)]
+
+
+class ActGradDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("n", ctypes.c_int64), ("type", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("reserved", ctypes.c_int32), ("offsets", ctypes.c_void_p),
+                ("dy", ctypes.c_void_p), ("lddy", ctypes.c_int64), ("z", ctypes.c_void_p), ("ldz", ctypes.c_int64),
+                ("dz", ctypes.c_void_p), ("lddz", ctypes.c_int64),
+                ("bias_grad", ctypes.c_void_p), ("stride_bias_grad", ctypes.c_int64)]
 
 
 class Plan(ctypes.Structure):
@@ -117,6 +151,12 @@ def load_library(path: str = None) -> ctypes.CDLL:
         "gdy_plan": (i32, [P, ctypes.POINTER(GemmDesc), i32, i32, i32, ctypes.POINTER(Plan)]),
         "gdy_execute": (i32, [P, ctypes.POINTER(GemmDesc), i32, i32, i32, P, ctypes.POINTER(Plan)]),
         "gdy_execute_static": (i32, [P, ctypes.POINTER(GemmDesc), i32, i32, i32, P, ctypes.POINTER(Plan)]),
+        "gdy_execute_epilogue": (i32, [P, ctypes.POINTER(GemmDesc), ctypes.POINTER(EpilogueDesc), i32, i32, i32, P,
+                                       ctypes.POINTER(Plan)]),
+        "gdy_execute_epilogue_static": (i32, [P, ctypes.POINTER(GemmDesc), ctypes.POINTER(EpilogueDesc), i32, i32,
+                                              i32, P, ctypes.POINTER(Plan)]),
+        "gdy_execute_grouped": (i32, [P, ctypes.POINTER(GroupedDesc), ctypes.POINTER(EpilogueDesc), P]),
+        "gdy_execute_act_grad": (i32, [P, ctypes.POINTER(ActGradDesc), P]),
         "gdy_set_timing": (i32, [P, i32]),
         "gdy_last_kernel_times": (i32, [P, ctypes.POINTER(ctypes.c_float),
                                         ctypes.POINTER(ctypes.c_float), i32]),
@@ -196,6 +236,189 @@ class Add:
         return d
 
 
+def _act(act) -> int:
+    if isinstance(act, str):
+        if act not in ACTS:
+            raise ValueError(f"unknown activation {act!r}: one of {', '.join(ACTS)}")
+        return ACTS[act]
+    return int(act)
+
+
+def _rows_of(t, name):
+    """A matrix's leading dimension; its rows must be contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must have a contiguous last dimension")
+    return max(t.stride(0), 1)
+
+
+def _check_offsets(offsets):
+    import torch
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.shape[0] < 1:
+        raise ValueError("offsets must be a contiguous int32 vector of groups + 1 values")
+    return offsets.shape[0] - 1
+
+
+def _bias_grad_stride(t, n, items):
+    """bias_grad: fp32, n values (summed over the items) or items x n."""
+    import torch
+    if t.dtype != torch.float32:
+        raise ValueError("bias_grad must be fp32")
+    if t.dim() == 1 and tuple(t.shape) == (n,) and (n < 2 or t.stride(0) == 1):
+        return 0
+    if t.dim() == 2 and tuple(t.shape) == (items, n) and (n < 2 or t.stride(1) == 1):
+        return t.stride(0) if items > 1 else 0
+    raise ValueError(f"bias_grad must hold {n} or {items} x {n} values, rows contiguous")
+
+
+@dataclass
+class Epilogue:
+    """What a GEMM does with its sums before their rounding (gdy_epilogue):
+    z = sums + bias, aux = z, C = act(z) + residual; with grad, from the saved
+    pre-activation aux, C = (sums + bias) * act'(aux) + residual.
+
+    bias: N values of C's type or fp32 (batch x N, or groups x N: one for each
+    item).  residual, aux: of C's shape and type.  bias_grad: fp32, overwritten with
+    the column sums of the unrounded C (N values, or batch x N / groups x N).
+    act: none, relu, gelu, gelu_tanh or silu."""
+    bias: object = None
+    act: object = "none"
+    residual: object = None
+    aux: object = None
+    grad: bool = False
+    bias_grad: object = None
+
+    def desc(self, c, items: int = 0) -> EpilogueDesc:
+        """For the output tensor c; items: batch items of a 3-D c, or the groups
+        that bias and bias_grad may be given for."""
+        e = EpilogueDesc()
+        e.act, e.grad = _act(self.act), int(bool(self.grad))
+        n = c.shape[-1]
+        if self.bias is not None:
+            b = self.bias
+            if tuple(b.shape) == (n,):
+                e.stride_bias = 0
+            elif items and tuple(b.shape) == (items, n):
+                e.stride_bias = b.stride(0) if items > 1 else 0
+            else:
+                raise ValueError(f"bias must hold {n} values" + (f" or {items} x {n}" if items else ""))
+            if n > 1 and b.stride(-1) != 1:
+                raise ValueError("bias must be contiguous")
+            e.bias, e.bias_type = b.data_ptr(), _dtype_code(b)
+        for name, ld, stride in (("residual", "ldr", "stride_r"), ("aux", "ldaux", "stride_aux")):
+            t = getattr(self, name)
+            if t is None:
+                continue
+            if t.dtype != c.dtype or tuple(t.shape) != tuple(c.shape):
+                raise ValueError(f"{name} must have C's shape and type")
+            setattr(e, name, t.data_ptr())
+            setattr(e, ld, _rows_of(t[0] if t.dim() == 3 else t, name) if t.dim() == 2 or t.shape[0] else 1)
+            setattr(e, stride, t.stride(0) if t.dim() == 3 else 0)
+        if self.bias_grad is not None:
+            e.stride_bias_grad = _bias_grad_stride(self.bias_grad, n, max(items, 1))
+            e.bias_grad = self.bias_grad.data_ptr()
+        return e
+
+
+@dataclass
+class Grouped:
+    """One product grouped by expert (gdy_grouped).  The rows of a are sorted by
+    group, group e holding rows offsets[e] to offsets[e + 1] (int32, on the device).
+
+    over "rows": c (rows x N) = a (rows x K) times b[e] (groups x K x N, or groups x
+    N x K with trans_b).  over "k": c[e] (groups x K x N) = a[e]^T b[e], the rows of e
+    of a (rows x K) and b (rows x N).  scales: one fp32 scale a group (fp8)."""
+    a: object
+    b: object
+    c: object
+    offsets: object
+    over: str = "rows"
+    trans_b: int = 0
+    scale_a: float = 1.0
+    scale_b: float = 1.0
+    scales: object = None
+    epilogue: object = None
+
+    def descs(self):
+        """(GroupedDesc, EpilogueDesc or None)."""
+        import torch
+        a, b, c = self.a, self.b, self.c
+        d = GroupedDesc()
+        groups = d.groups = _check_offsets(self.offsets)
+        if self.over not in ("rows", "k"):
+            raise ValueError("over must be 'rows' or 'k'")
+        over_k = self.over == "k"
+        d.over = OVER_K if over_k else OVER_ROWS
+        per_group = c if over_k else b
+        if per_group.dim() != 3 or per_group.shape[0] != groups:
+            raise ValueError(f"{'c' if over_k else 'b'} must be a 3-D tensor of {groups} groups")
+        if a.dim() != 2 or (b if over_k else c).dim() != 2:
+            raise ValueError("the row matrices must be 2-D")
+        d.rows, d.k = a.shape
+        d.trans_b = int(self.trans_b)
+        if over_k:
+            d.n = b.shape[1]
+            ok = b.shape[0] == d.rows and tuple(c.shape[1:]) == (d.k, d.n)
+        else:
+            d.n = c.shape[1]
+            ok = c.shape[0] == d.rows and tuple(b.shape[1:]) == ((d.n, d.k) if d.trans_b else (d.k, d.n))
+        if not ok:
+            raise ValueError(f"shapes disagree: a {tuple(a.shape)}, b {tuple(b.shape)}, c {tuple(c.shape)}")
+        d.a_type, d.b_type, d.c_type = _dtype_code(a), _dtype_code(b), _dtype_code(c)
+        d.offsets = self.offsets.data_ptr()
+
+        def item(t, name):
+            if t.dim() == 3:
+                return (_rows_of(t[0], name) if groups else 1), t.stride(0)
+            return _rows_of(t, name), 0
+        d.a, (d.lda, _) = a.data_ptr(), item(a, "a")
+        d.b, (d.ldb, d.stride_b) = b.data_ptr(), item(b, "b")
+        d.c, (d.ldc, d.stride_c) = c.data_ptr(), item(c, "c")
+        d.scale_a, d.scale_b = float(self.scale_a), float(self.scale_b)
+        if self.scales is not None:
+            if self.scales.dtype != torch.float32 or tuple(self.scales.shape) != (groups,) or \
+                    not self.scales.is_contiguous():
+                raise ValueError("scales must hold one fp32 value a group")
+            d.scales = self.scales.data_ptr()
+        return d, (None if self.epilogue is None else self.epilogue.desc(c, groups))
+
+
+@dataclass
+class ActGrad:
+    """dz = dy * act'(z) and bias_grad = the column sums of dy * act'(z) (gdy_act_grad),
+    over all rows, or with offsets (int32, groups + 1) over the rows of each group.
+    z may be None where act is none; dz or bias_grad may be None."""
+    dy: object
+    z: object = None
+    dz: object = None
+    bias_grad: object = None
+    act: object = "none"
+    offsets: object = None
+
+    def desc(self) -> ActGradDesc:
+        d = ActGradDesc()
+        if self.dy.dim() != 2:
+            raise ValueError("dy must be 2-D")
+        d.rows, d.n = self.dy.shape
+        d.type, d.act = _dtype_code(self.dy), _act(self.act)
+        if d.act != ACT_NONE and self.z is None:
+            raise ValueError("an activation needs z")
+        for name in ("dy", "z", "dz"):
+            t = getattr(self, name)
+            if t is None:
+                continue
+            if t.dtype != self.dy.dtype or tuple(t.shape) != tuple(self.dy.shape):
+                raise ValueError(f"{name} must have dy's shape and type")
+            setattr(d, name, t.data_ptr())
+            setattr(d, "ld" + name, _rows_of(t, name))
+        if self.offsets is not None:
+            d.groups = _check_offsets(self.offsets)
+            d.offsets = self.offsets.data_ptr()
+        if self.bias_grad is not None:
+            d.stride_bias_grad = _bias_grad_stride(self.bias_grad, d.n, max(d.groups, 1))
+            d.bias_grad = self.bias_grad.data_ptr()
+        return d
+
+
 @dataclass
 class Gemm:
     """One GEMM of a submission, from torch device tensors.
@@ -204,7 +427,8 @@ class Gemm:
     trans_b); c: M x N output.  Strided 2-D views are allowed as long as the
     last dimension is contiguous (ld = stride(0)).  A strided batch
     (B-GEMM) passes 3-D tensors whose first dimension is the batch: C must
-    be 3-D; A or B may stay 2-D to be shared by every item (stride 0)."""
+    be 3-D; A or B may stay 2-D to be shared by every item (stride 0).
+    epilogue: an Epilogue, or None."""
     a: object
     b: object
     c: object
@@ -214,6 +438,7 @@ class Gemm:
     scale_b: float = 1.0
     tenant: int = 0
     variant: int = -1
+    epilogue: object = None
 
     def desc(self) -> GemmDesc:
         a, b, c = self.a, self.b, self.c
@@ -259,6 +484,19 @@ def descs(gemms) -> ctypes.Array:
     return arr
 
 
+def epilogue_descs(gemms):
+    """The epilogues of a submission as a C array beside descs(gemms), or None
+    where no member has one."""
+    if not any(getattr(g, "epilogue", None) is not None for g in gemms):
+        return None
+    arr = (EpilogueDesc * max(len(gemms), 1))()
+    for i, g in enumerate(gemms):
+        e = getattr(g, "epilogue", None)
+        if e is not None:
+            arr[i] = e.desc(g.c, g.c.shape[0] if g.c.dim() == 3 else 0)
+    return arr
+
+
 class Context:
     """A libgdy context on one device (see gdy_create)."""
 
@@ -300,27 +538,57 @@ class Context:
 
     def execute(self, gemms, mode="selector", forced_cd: int = 0, stream=None, want_plan=False):
         """Launch a submission on `stream` (torch stream, raw handle or None for
-        torch's current stream).  Returns the plan dict when want_plan."""
-        arr = descs(gemms)
+        torch's current stream).  Returns the plan dict when want_plan.  Gemm
+        objects may carry epilogues."""
+        arr, eps = descs(gemms), epilogue_descs(gemms)
         handle = _stream_handle(stream)
         p = Plan()
-        self._check(self.lib.gdy_execute(self.h, arr, len(gemms), _mode(mode), forced_cd,
-                                         handle, ctypes.byref(p)))
+        if eps is None:
+            self._check(self.lib.gdy_execute(self.h, arr, len(gemms), _mode(mode), forced_cd,
+                                             handle, ctypes.byref(p)))
+        else:
+            self._check(self.lib.gdy_execute_epilogue(self.h, arr, eps, len(gemms), _mode(mode), forced_cd,
+                                                      handle, ctypes.byref(p)))
         return p.as_dict() if want_plan else None
 
     def execute_static(self, gemms, mode="selector", forced_cd: int = 0, stream=None, want_plan=False):
         """gdy_execute_static: as execute(), with the split-K planes in the
         library's static device array (no allocation)."""
-        arr = descs(gemms)
+        arr, eps = descs(gemms), epilogue_descs(gemms)
         handle = _stream_handle(stream)
         p = Plan()
-        self._check(self.lib.gdy_execute_static(self.h, arr, len(gemms), _mode(mode), forced_cd,
-                                                handle, ctypes.byref(p)))
+        if eps is None:
+            self._check(self.lib.gdy_execute_static(self.h, arr, len(gemms), _mode(mode), forced_cd,
+                                                    handle, ctypes.byref(p)))
+        else:
+            self._check(self.lib.gdy_execute_epilogue_static(self.h, arr, eps, len(gemms), _mode(mode), forced_cd,
+                                                             handle, ctypes.byref(p)))
         return p.as_dict() if want_plan else None
 
-    def execute_descs(self, arr, n, mode, forced_cd, handle):
-        """Launch prepared GemmDesc arrays (no per-call marshalling)."""
-        self._check(self.lib.gdy_execute(self.h, arr, n, mode, forced_cd, handle, None))
+    def execute_descs(self, arr, n, mode, forced_cd, handle, epilogues=None):
+        """Launch prepared GemmDesc arrays (no per-call marshalling); epilogues: as
+        epilogue_descs() makes them."""
+        if epilogues is None:
+            self._check(self.lib.gdy_execute(self.h, arr, n, mode, forced_cd, handle, None))
+        else:
+            self._check(self.lib.gdy_execute_epilogue(self.h, arr, epilogues, n, mode, forced_cd, handle, None))
+
+    def execute_grouped(self, product: Grouped, stream=None):
+        """Launch a product grouped by expert (gdy_execute_grouped)."""
+        self.execute_grouped_descs(*product.descs(), _stream_handle(stream))
+
+    def execute_grouped_descs(self, desc, epilogue, handle):
+        """Launch a prepared GroupedDesc (epilogue: an EpilogueDesc or None)."""
+        self._check(self.lib.gdy_execute_grouped(self.h, ctypes.byref(desc),
+                                                 None if epilogue is None else ctypes.byref(epilogue), handle))
+
+    def execute_act_grad(self, op: ActGrad, stream=None):
+        """Launch an activation and bias gradient (gdy_execute_act_grad)."""
+        self.execute_act_grad_desc(op.desc(), _stream_handle(stream))
+
+    def execute_act_grad_desc(self, desc, handle):
+        """Launch a prepared ActGradDesc."""
+        self._check(self.lib.gdy_execute_act_grad(self.h, ctypes.byref(desc), handle))
 
     def set_rc(self, budget_cus: int):
         self._check(self.lib.gdy_set_rc(self.h, budget_cus))
