@@ -155,7 +155,7 @@ def run_epilogue(ctx, gemms, epilogues, mode=gdy.SELECTOR, static=False):
     ({}, {"residual": BASE + (4 << 24) + 1}, UNSUPPORTED), ({}, {"aux": BASE + (5 << 24) + 1}, UNSUPPORTED),
     ({}, {"bias_grad": BASE + (6 << 24) + 2}, UNSUPPORTED),
     ({}, {"grad": 1, "aux": None}, INVALID), ({}, {"grad": 1, "aux": None, "act": 0}, OK),
-    ({}, {"ldr": 1 << 22, "residual": 1 << 40}, OK), ({}, {"ldr": 1 << 23}, UNSUPPORTED), ({}, {"ldaux": 1 << 23}, UNSUPPORTED),
+    ({}, {"ldr": 1 << 21, "residual": 1 << 40}, OK), ({}, {"ldr": 1 << 23}, UNSUPPORTED), ({}, {"ldaux": 1 << 23}, UNSUPPORTED),
     # C over its own residual, and over the pre-activation it replaces; nothing else overlaps
     ({}, {"residual": BASE + (2 << 24)}, OK), ({}, {"residual": BASE + (2 << 24) + 2}, ALIAS),
     ({}, {"residual": BASE + (2 << 24), "ldr": 100}, ALIAS),
