@@ -16,6 +16,7 @@ LIB = os.path.join(HERE, "libgdy.so")
 
 SOURCES = ["kernels_joint_bf16.hip", "kernels_joint_f16.hip", "kernels_joint_fp8.hip", "kernels_joint_f32.hip",
            "kernels_ep_bf16.hip", "kernels_ep_f16.hip", "kernels_ep_fp8.hip", "kernels_ep_f32.hip",
+           "kernels_ep1_bf16.hip", "kernels_ep1_f16.hip", "kernels_ep1_fp8.hip", "kernels_ep1_f32.hip",
            "kernels_group_bf16.hip", "kernels_group_f16.hip", "kernels_group_fp8.hip", "kernels_group_f32.hip",
            "kernels_d_bf16.hip", "kernels_d_f16.hip", "kernels_d_fp8.hip",
            "kernels_bf16.hip", "kernels_f16.hip", "kernels_fp8.hip", "kernels_f32.hip", "kernels_ew.hip",

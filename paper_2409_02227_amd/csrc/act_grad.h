@@ -86,11 +86,11 @@ __global__ void __launch_bounds__(256) act_grad(KActGrad g) {
         const int r = r0 + u * RP;
         if (r >= m) break;
         float x[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) x[q] = y[u].get(q);
+        y[u].get(x);
         if (g.z) {
-#pragma unroll
-          for (int q = 0; q < 8; ++q) x[q] *= act_slope(z[u].get(q), g.act);
+          float v[8];
+          z[u].get(v);
+          apply_slopes(x, v, g.act);
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum[q] += x[q];

@@ -4,15 +4,17 @@
 //   g = (scale * sum + bias(j)) * f'(aux(i,j));   C = round(g + R(i,j))
 // and the column sums of the unrounded C, from which bias gradients are made.
 //
-// The accumulators of a tile go through LDS as fp32 rows (64 or 128 at a time,
-// which the operand stages they replace have room for), so that a lane owns
-// eight consecutive columns of whole rows: the residual and the saved
-// pre-activation are read, and C written, with 16 consecutive bytes a lane, the
-// bias stays in registers, and one rolled loop holds the activations, where the
-// accumulators' order would need them unrolled over every block.  Nothing is
-// rounded between the sum and C.
+// Each wave passes its accumulators through LDS of its own as fp32 rows (32 or 64
+// at a time, in the room of the operand stages), so that a lane owns eight
+// consecutive columns: the residual and the saved pre-activation are read, and C
+// written, with 16 consecutive bytes a lane, the bias stays in registers, and one
+// rolled loop holds the activations, where the accumulators' order would need them
+// unrolled over every block.  Nothing is rounded between the sum and C.  No barrier
+// separates the waves, so that one's arithmetic runs beside another's stores.
 #pragma once
 #include <stddef.h>
+
+#include <type_traits>
 
 #include "lds_copy.h"
 
@@ -41,8 +43,10 @@ struct NoEpi {
 // tile's sums are done: the empty asm hides the pointer's origin from the compiler
 // there, which would otherwise load the fields before the tile loop and keep them
 // in registers through it (scalars then spill to scratch memory).
-struct MemberEpi {
+// AHEAD: the rows whose residual and saved pre-activation a wave loads together.
+template <int AHEAD> struct MemberEpi {
   static constexpr bool on = true;
+  static constexpr int ahead = AHEAD;
   typedef const __attribute__((address_space(4))) uint8_t* Ptr;
   int gi;
   __device__ __forceinline__ EpiOut operator()(int item, int tile_row) const {
@@ -68,8 +72,9 @@ struct MemberEpi {
 // ---- activations --------------------------------------------------------------
 constexpr float kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ float logistic(float x) {  // 1 / (1 + e^-x); 0 where e^-x overflows
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x));
+// 1 / (1 + 2^y): the logistic function of -y / log2(e); 0 where 2^y overflows.
+__device__ __forceinline__ float logistic2(float y) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y));
 }
 
 // exp(-x^2 / 2) and Phi(x), the normal distribution function.  With a = |x|,
@@ -93,43 +98,65 @@ __device__ __forceinline__ float normal_cdf(float x, float& bell) {
   return x < 0.0f ? q : 1.0f - q;
 }
 
-constexpr float kTanhA = 1.5957691216057308f;              // 2 sqrt(2 / pi)
-constexpr float kTanhB = 1.5957691216057308f * 0.044715f;  // (1 + tanh u) / 2 = logistic(2u)
+// (1 + tanh u) / 2 = logistic(2u), 2u = x (A + B x^2)
+constexpr float kTanhA = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+constexpr float kTanhB = 1.5957691216057308f * 0.044715f;
 
-__device__ __forceinline__ float act_value(float x, int act) {
-  switch (act) {
-    case ACT_RELU: return x < 0.0f ? 0.0f : x;  // NaN stays NaN
-    case ACT_GELU: {
-      float bell;
-      return x * normal_cdf(x, bell);
-    }
-    case ACT_GELU_TANH: return x * logistic(x * __builtin_fmaf(kTanhB, x * x, kTanhA));
-    case ACT_SILU: return x * logistic(x);
-    default: return x;
+template <int ACT> __device__ __forceinline__ float act_value(float x) {
+  if constexpr (ACT == ACT_RELU) return x < 0.0f ? 0.0f : x;  // NaN stays NaN
+  if constexpr (ACT == ACT_GELU) {
+    float bell;
+    return x * normal_cdf(x, bell);
   }
+  if constexpr (ACT == ACT_GELU_TANH) return x * logistic2(x * __builtin_fmaf(-kLog2e * kTanhB, x * x, -kLog2e * kTanhA));
+  if constexpr (ACT == ACT_SILU) return x * logistic2(-kLog2e * x);
+  return x;
 }
 
 // f'(x).  Beyond +-64 every slope is 0 or 1 in fp32; the saved value may be
 // infinite where it passed its type's range, and inf * 0 must not enter.
-__device__ __forceinline__ float act_slope(float x, int act) {
+template <int ACT> __device__ __forceinline__ float act_slope(float x) {
   x = x > 64.0f ? 64.0f : x < -64.0f ? -64.0f : x;
-  switch (act) {
-    case ACT_RELU: return x <= 0.0f ? 0.0f : 1.0f;
-    case ACT_GELU: {
-      float bell;
-      const float cdf = normal_cdf(x, bell);
-      return __builtin_fmaf(x * bell, 0.3989422804014327f, cdf);
-    }
-    case ACT_GELU_TANH: {
-      const float x2 = x * x, p = logistic(x * __builtin_fmaf(kTanhB, x2, kTanhA));
-      return __builtin_fmaf(x * p * (1.0f - p), __builtin_fmaf(3.0f * kTanhB, x2, kTanhA), p);
-    }
-    case ACT_SILU: {
-      const float p = logistic(x);
-      return __builtin_fmaf(x * p, 1.0f - p, p);
-    }
-    default: return 1.0f;
+  if constexpr (ACT == ACT_RELU) return x <= 0.0f ? 0.0f : 1.0f;
+  if constexpr (ACT == ACT_GELU) {
+    float bell;
+    const float cdf = normal_cdf(x, bell);
+    return __builtin_fmaf(x * bell, 0.3989422804014327f, cdf);
   }
+  if constexpr (ACT == ACT_GELU_TANH) {
+    const float x2 = x * x, p = logistic2(x * __builtin_fmaf(-kLog2e * kTanhB, x2, -kLog2e * kTanhA));
+    return __builtin_fmaf(x * p * (1.0f - p), __builtin_fmaf(3.0f * kTanhB, x2, kTanhA), p);
+  }
+  if constexpr (ACT == ACT_SILU) {
+    const float p = logistic2(-kLog2e * x);
+    return __builtin_fmaf(x * p, 1.0f - p, p);
+  }
+  return 1.0f;
+}
+
+// Eight values by the activation that the call names: one branch for all of them
+// (one for each cost more than the arithmetic: a 256 x 256 tile's bias alone 10 us).
+template <class F> __device__ __forceinline__ void by_act(int act, F f) {
+  switch (act) {
+    case ACT_RELU: f(std::integral_constant<int, ACT_RELU>()); break;
+    case ACT_GELU: f(std::integral_constant<int, ACT_GELU>()); break;
+    case ACT_GELU_TANH: f(std::integral_constant<int, ACT_GELU_TANH>()); break;
+    case ACT_SILU: f(std::integral_constant<int, ACT_SILU>()); break;
+  }
+}
+// x = f(x)
+__device__ __forceinline__ void apply_values(float (&x)[8], int act) {
+  by_act(act, [&](auto a) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] = act_value<decltype(a)::value>(x[q]);
+  });
+}
+// x *= f'(z)
+__device__ __forceinline__ void apply_slopes(float (&x)[8], const float (&z)[8], int act) {
+  by_act(act, [&](auto a) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] *= act_slope<decltype(a)::value>(z[q]);
+  });
 }
 
 // ---- eight consecutive columns of a row of C's type -----------------------------
@@ -149,6 +176,10 @@ template <int DT> struct Row8 {
       for (int e = 0; e < 8; ++e)
         if (e < left) w[e * OS / 16][(e * OS / 4) & 3] |= load_elem<OS>(r, off + e * OS) << ((e * OS * 8) & 31);
     }
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = get(e);
   }
   __device__ __forceinline__ float get(int e) const {
     const unsigned x = w[e * OS / 16][(e * OS / 4) & 3];
@@ -186,121 +217,144 @@ __device__ __forceinline__ void load_bias(const EpiOut& o, int j, float (&b)[8])
   for (int q = 0; q < 8; ++q) b[q] = 0.0f;
   if (!o.bias) return;
   if (o.bias_f32) {
-    const Rsrc r = make_rsrc(o.bias, o.n * 4);
+    Row8<DT_F32> w;
+    w.load(make_rsrc(o.bias, o.n * 4), j * 4, true, 8);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) b[q] = ew_decode<DT_F32>(load_elem<4>(r, (j + q) * 4));
+    for (int q = 0; q < 8; ++q) b[q] = w.get(q);
   } else {
     constexpr int OS = OutSize<DT>::v;
-    const Rsrc r = make_rsrc(o.bias, o.n * OS);
+    Row8<DT> w;
+    // whole dwords: the last element may share one with bytes past the bias
+    const bool dwords = ((uintptr_t)o.bias & 3) == 0;
+    w.load(make_rsrc(o.bias, dwords ? (o.n * OS + 3) & ~3 : o.n * OS), j * OS, dwords, 8);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) b[q] = ew_decode<Row8<DT>::OT>(load_elem<OS>(r, (j + q) * OS));
+    for (int q = 0; q < 8; ++q) b[q] = w.get(q);
   }
 }
 
-// One tile's epilogue, by the NT threads of a workgroup: the caller lays some of its
-// rows into LDS, PITCH bytes apart, and calls rows() between two barriers, until
-// all rows are done, then sums().
-template <int DT, int BN, int NT> struct EpiTile {
+// What a wave does with blocks of R rows x WC columns of a tile's sums, one after
+// another: the caller lays a block's sums into the wave's LDS, PITCH bytes a row, and
+// calls rows().  Lane l owns the columns 8 * (l % LPR) .. + 7.
+template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
   static constexpr int OS = OutSize<DT>::v;
-  static constexpr int LPR = BN / 8;       // lanes per row
-  static constexpr int RP = NT / LPR;      // rows per pass
-  static constexpr int PITCH = BN * 4 + 16;  // a half wave's 16 rows of 16 bytes on distinct banks
-  static constexpr int AHEAD = NT == 512 ? 2 : 4;  // rows whose residual and aux are loaded together
+  static constexpr int LPR = WC / 8;             // lanes per row
+  static constexpr int RP = 64 / LPR;            // rows per pass
+  static constexpr int PASSES = (R + RP - 1) / RP;
+  static constexpr int AHEAD = PASSES < ROWS_AHEAD ? PASSES : ROWS_AHEAD;
+  static_assert(PASSES % AHEAD == 0, "whole steps");
+  static constexpr int PITCH = WC * 4 + 16;      // writes of 16 rows of 16 bytes hit distinct banks
+  static constexpr int BYTES = R * PITCH;        // LDS of a wave
   const EpiOut o;
   Rsrc rc, rr, ra;
-  int c8, left;  // first column of this lane within the tile, and how many of its eight lie inside C
-  int n0, cols;  // the tile's first column, and how many of its columns lie inside C
-  int tid;
+  int lane;
+  int col, left;  // this lane's first column, and how many of its eight lie inside C
   bool grad;
   float b[8], sum[8];
 
-  __device__ __forceinline__ EpiTile(const EpiOut& out, int n0_, int tid_) : o(out), n0(n0_), tid(tid_) {
-    cols = min(BN, o.n - n0);
+  __device__ __forceinline__ EpiWave(const EpiOut& out, int lane_) : o(out), lane(lane_) {
     rc = make_rsrc(o.c, o.c_bytes);
     rr = make_rsrc(o.res, o.res ? ((o.m - 1) * o.ldr + o.n) * OS : 0);
     ra = make_rsrc(o.aux, o.aux ? ((o.m - 1) * o.ldaux + o.n) * OS : 0);
-    c8 = (tid % LPR) * 8;
-    left = cols - c8;
     grad = o.grad && o.act != ACT_NONE;
-    load_bias<DT>(o, n0 + c8, b);
+  }
+  // the blocks from here on start at column `first` of C
+  __device__ __forceinline__ void columns(int first) {
+    col = first + (lane % LPR) * 8;
+    left = o.n - col;
+    load_bias<DT>(o, col, b);
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum[q] = 0.0f;
   }
 
   __device__ __forceinline__ void load_inputs(int row, Row8<DT>& res, Row8<DT>& aux) {
-    const int col = (n0 + c8) * OS;
-    if (o.res) res.load(rr, row * o.ldr * OS + col, OS == 4 || o.res_vec, left);
-    if (grad) aux.load(ra, row * o.ldaux * OS + col, OS == 4 || o.aux_vec, left);
+    if (o.res) res.load(rr, (row * o.ldr + col) * OS, OS == 4 || o.res_vec, left);
+    if (grad) aux.load(ra, (row * o.ldaux + col) * OS, OS == 4 || o.aux_vec, left);
   }
 
   // Eight sums of a row to C.
   __device__ __forceinline__ void finish(int row, float (&x)[8], const Row8<DT>& res, const Row8<DT>& aux) {
-    const int col = (n0 + c8) * OS;
     Row8<DT> w;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) x[q] = x[q] * o.scale + b[q];
+    for (int q = 0; q < 8; ++q) x[q] = DT == DT_FP8 ? __builtin_fmaf(x[q], o.scale, b[q]) : x[q] + b[q];
     if (grad) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) x[q] *= act_slope(aux.get(q), o.act);
+      float z[8];
+      aux.get(z);
+      apply_slopes(x, z, o.act);
     } else if (!o.grad) {
       if (o.aux) {
         w.set(x);
-        w.store(ra, row * o.ldaux * OS + col, OS == 4 || o.aux_vec, left);
+        w.store(ra, (row * o.ldaux + col) * OS, OS == 4 || o.aux_vec, left);
       }
-#pragma unroll
-      for (int q = 0; q < 8; ++q) x[q] = act_value(x[q], o.act);
+      apply_values(x, o.act);
     }
     if (o.res) {
 #pragma unroll
       for (int q = 0; q < 8; ++q) x[q] += res.get(q);
     }
+    if (o.part) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sum[q] += x[q];
+      for (int q = 0; q < 8; ++q) sum[q] += x[q];
+    }
     w.set(x);
-    w.store(rc, row * o.ldc * OS + col, OS == 4 || o.c_vec, left);
+    w.store(rc, (row * o.ldc + col) * OS, OS == 4 || o.c_vec, left);
   }
 
-  // The rows 0 .. count - 1 at `rows_lds`: rows m0, m0 + 1, ... of C.
-  __device__ __forceinline__ void rows(const lds_u8* rows_lds, int m0, int count) {
-    if (left <= 0) return;
-    for (int r0 = tid / LPR; r0 < count; r0 += RP * AHEAD) {
+  // The block at `block`: rows m0, m0 + 1, ... of C, which has `inside` from m0 on.
+  __device__ __forceinline__ void rows(const lds_u8* block, int m0, int inside) {
+    const int count = min(R, inside);  // a pass may reach past a block of 16 rows
+    // the wave's own sums, in LDS in the order of its instructions
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int u0 = 0; u0 < PASSES; u0 += AHEAD) {
       Row8<DT> res[AHEAD], aux[AHEAD];
+      const int r0 = lane / LPR + u0 * RP;
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
-        if (r0 + u * RP < count) load_inputs(m0 + r0 + u * RP, res[u], aux[u]);
+        if (r0 + u * RP < count && left > 0) load_inputs(m0 + r0 + u * RP, res[u], aux[u]);
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         const int r = r0 + u * RP;
-        if (r >= count) break;
-        const lds_u8* at = rows_lds + r * PITCH + c8 * 4;
-        const f32x4 lo = *(const __attribute__((address_space(3))) f32x4*)at;
-        const f32x4 hi = *(const __attribute__((address_space(3))) f32x4*)(at + 16);
-        float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        finish(m0 + r, x, res[u], aux[u]);
+        if (r < count && left > 0) {
+          const lds_u8* at = block + r * PITCH + (lane % LPR) * 32;
+          const f32x4 lo = *(const __attribute__((address_space(3))) f32x4*)at;
+          const f32x4 hi = *(const __attribute__((address_space(3))) f32x4*)(at + 16);
+          float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          finish(m0 + r, x, res[u], aux[u]);
+        }
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next block's sums
+    __builtin_amdgcn_wave_barrier();
   }
 
-  // The tile's column sums to its row of part.  Lanes add their rows in ascending
-  // order, then the row groups are added in order: the result does not depend on
-  // the run.  `lds` holds NT * 8 floats and no rows that are still read.
-  __device__ __forceinline__ void sums(lds_u8* lds) {
+  // This lane's sums of its eight columns to LDS: row `r0` (of its RP) of a table of
+  // `width` columns, the lane's at `c`.
+  __device__ __forceinline__ void put_sums(lds_u8* table, int row, int width, int c) const {
     typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-    lds_u8* at = lds + (tid / LPR) * (BN * 4) + c8 * 4;
+    lds_u8* at = table + (row * width + c) * 4;
     *(lds_f32x4*)at = f32x4{sum[0], sum[1], sum[2], sum[3]};
     *(lds_f32x4*)(at + 16) = f32x4{sum[4], sum[5], sum[6], sum[7]};
-    __syncthreads();
-    if (tid < cols) {
-      float x = 0.0f;
-#pragma unroll 4
-      for (int r = 0; r < RP; ++r) x += *(const __attribute__((address_space(3))) float*)(lds + r * (BN * 4) + tid * 4);
-      o.part[n0 + tid] = x;
-    }
   }
 };
 
+// The table of column sums that the waves have laid down (`rows` rows of `width`) to
+// part: lanes added their rows in ascending order, the table's rows are added in
+// order, so the result does not depend on the run.
+template <int ROWS>
+__device__ __forceinline__ void add_sums(const lds_u8* table, int width, float* part, int cols, int tid) {
+  if (tid < cols) {
+    float x = 0.0f;
+#pragma unroll 8
+    for (int r = 0; r < ROWS; ++r)
+      x += *(const __attribute__((address_space(3))) float*)(table + (r * width + tid) * 4);
+    part[tid] = x;
+  }
+}
+
 // ---- split-K reduction with an epilogue -------------------------------------------
-// As split_reduce, kEpiReduceRows rows x 128 columns a tile: 256 threads of eight columns.
+// As split_reduce, kEpiReduceRows rows x 128 columns a tile: 256 threads of eight
+// columns, a wave four rows.
 template <int DT>
 __global__ void __launch_bounds__(256) split_reduce_ep(KLaunch L, KEpis E) {
   (void)E;  // read by MemberEpi
@@ -310,7 +364,7 @@ __global__ void __launch_bounds__(256) split_reduce_ep(KLaunch L, KEpis E) {
   const KArgs& p = L.g[gi];
   const int wg0 = L.first[gi];
   const int nwg = L.first[gi + 1] - wg0;
-  typedef EpiTile<DT, BN, 256> Tile;
+  typedef EpiWave<DT, 4, BN, 1> Wave;
   const int tid = threadIdx.x;
   const int M = (int)p.m, N = (int)p.n, S = p.split;
   const int tn = (N + BN - 1) / BN, tm = (M + kEpiReduceRows - 1) / kEpiReduceRows;
@@ -318,12 +372,13 @@ __global__ void __launch_bounds__(256) split_reduce_ep(KLaunch L, KEpis E) {
   const size_t plane = (size_t)M * (size_t)N;
   for (int tb = (int)blockIdx.x - wg0; tb < total; tb += nwg) {
     const int item = tb / ntiles, t = tb - item * ntiles;
-    const int row = (t / tn) * kEpiReduceRows + tid / Tile::LPR;
-    Tile x(MemberEpi{gi}(item, t / tn), (t % tn) * BN, tid);
+    const int row = (t / tn) * kEpiReduceRows + tid / Wave::LPR, n0 = (t % tn) * BN;
+    Wave x(MemberEpi<1>{gi}(item, t / tn), tid & 63);
+    x.columns(n0);
     if (row < M && x.left > 0) {
       Row8<DT> res, aux;
       x.load_inputs(row, res, aux);
-      const float* P = p.ws + (size_t)item * S * plane + (size_t)row * N + x.n0 + x.c8;
+      const float* P = p.ws + (size_t)item * S * plane + (size_t)row * N + x.col;
       float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
       if ((N & 3) == 0 && x.left >= 8) {  // 16-byte aligned rows of the planes
         for (int s = 0; s < S; ++s) {
@@ -341,7 +396,9 @@ __global__ void __launch_bounds__(256) split_reduce_ep(KLaunch L, KEpis E) {
       x.finish(row, v, res, aux);
     }
     if (x.o.part) {
-      x.sums((lds_u8*)smem);
+      x.put_sums((lds_u8*)smem, tid / Wave::LPR, BN, (tid % Wave::LPR) * 8);
+      __syncthreads();
+      add_sums<kEpiReduceRows>((lds_u8*)smem, BN, x.o.part + n0, min(BN, N - n0), tid);
       __syncthreads();  // the next tile's sums overwrite these
     }
   }

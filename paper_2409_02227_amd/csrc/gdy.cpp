@@ -1545,6 +1545,11 @@ const void* epilogue_kernel(int dtype, int family) {
          : dtype == DT_FP8 ? ep_fp8(family) : dtype == DT_F32 ? ep_f32(family) : nullptr;
 }
 
+const void* lone_epilogue_kernel(int dtype, int family, int code, bool copies) {
+  return dtype == DT_BF16 ? ep_lone_bf16(family, code, copies) : dtype == DT_F16 ? ep_lone_f16(family, code, copies)
+         : dtype == DT_FP8 ? ep_lone_fp8(family, code, copies) : ep_lone_f32(family, code, copies);
+}
+
 // Rows of partial column sums that an item of g may take: its tile rows, or those
 // of the split reduction.  Members of 256 x 256 kernels may run 128-row tiles.
 int64_t part_rows(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
@@ -1848,14 +1853,21 @@ gdy_status launch_epilogues(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue*
   KEpis epis;
   BiasSums sums;
   sums.count = 0;
-  bool any_sums = false;
+  bool any_sums = false, one_code = true, copies = true;
+  int code = -1;
   for (int u = 0; u < launch.count; ++u) {
     const int i = members[u];
+    if (!launch.g[u].ew) {
+      one_code = one_code && (code < 0 || code == launch.g[u].code);
+      code = launch.g[u].code;
+      copies = copies && launch.g[u].a_dma && launch.g[u].b_dma;
+    }
     epis.e[u] = make_epi(g[i], ep[i], launch.g[u], part_off[i] >= 0 ? ws_base + part_off[i] / 4 : nullptr);
     any_sums = any_sums || ep[i].bias_grad;
   }
   void* argv[] = {(void*)&launch, &epis};
-  hipError_t e = hipExtLaunchKernel(epilogue_kernel(dtype, family), dim3(grid), dim3(family == 1 ? 256 : 512), argv, 0,
+  const void* func = one_code ? lone_epilogue_kernel(dtype, family, code, copies) : epilogue_kernel(dtype, family);
+  hipError_t e = hipExtLaunchKernel(func, dim3(grid), dim3(family == 1 ? 256 : 512), argv, 0,
                                     hs, start, !split && !any_sums ? stop : nullptr, 0);
   if (e == hipSuccess && split) {
     KLaunch red;

@@ -228,6 +228,11 @@ const void* ep_bf16(int family);
 const void* ep_f16(int family);
 const void* ep_fp8(int family);
 const void* ep_f32(int family);
+// For launches whose members share a joint code; copies: all of them take copies.
+const void* ep_lone_bf16(int family, int code, bool copies);
+const void* ep_lone_f16(int family, int code, bool copies);
+const void* ep_lone_fp8(int family, int code, bool copies);
+const void* ep_lone_f32(int family, int code, bool copies);
 GroupKernel group_bf16(int over_k, int tb, int tile);
 GroupKernel group_f16(int over_k, int tb, int tile);
 GroupKernel group_fp8(int over_k, int tb, int tile);

@@ -106,7 +106,8 @@ template <int ES, bool KC, bool SPILLS> struct PhaseCopy {
 };
 
 // The tiles of one member (work items lwg, lwg + nwg, ... of p), in the kPLds
-// bytes at smem.  EP: where the results go (NoEpi: to C, scaled and rounded).
+// bytes at smem.  EP: where the results go (NoEpi: to C, scaled and rounded); with an
+// epilogue, work item lwg alone.
 template <int DT, int TA, int TB, bool JOINT, class EP = NoEpi>
 __device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds_u8* smem, EP ep = EP()) {
   const Args<JOINT> own(args);
@@ -279,35 +280,43 @@ __device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds
     // two rows an instruction, where the accumulators' own order gives 32.
     // The 528-byte row pitch keeps a half wave's 16 rows of 16 bytes on
     // distinct banks.
-    if constexpr (EP::on) {  // fp32 rows, a half of the tile at a time (133 of the 144 KiB)
-      typedef EpiTile<DT, 256, 512> Epi;
-      static_assert(128 * Epi::PITCH <= kPLds, "half of the tile fits in the ring");
-      Epi x(ep(item, tm), n0, (int)threadIdx.x);
-      auto dump = [&](const Acc (&h)[2][2][4]) {
+    if constexpr (EP::on) {  // a wave's quadrants one after another, by columns
+      typedef EpiWave<DT, 64, 32, EP::ahead> Epi;
+      static_assert(8 * Epi::BYTES + 2 * Epi::RP * 256 * 4 <= kPLds, "blocks and sums fit in the ring");
+      Epi x(ep(item, tm), lane);
+      lds_u8* block = smem + wave * Epi::BYTES;
+      auto dump = [&](const Acc (&h)[2][4]) {
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              *(__attribute__((address_space(3))) f32x4*)(smem + (wm * 64 + i * 16 + (lane & 15)) * Epi::PITCH +
-                                                          (hb * 128 + wn * 32 + j * 16 + 4 * (lane >> 4)) * 4) =
-                  h[hb][j][i];
+          for (int j = 0; j < 2; ++j)
+            *(__attribute__((address_space(3))) f32x4*)(block + (i * 16 + (lane & 15)) * Epi::PITCH +
+                                                        (j * 16 + 4 * (lane >> 4)) * 4) = h[j][i];
+      };
+      lds_u8* table = smem + 8 * Epi::BYTES;
+      auto put_sums = [&](int hb) {
+        x.put_sums(table, wm * Epi::RP + lane / Epi::LPR, 256, hb * 128 + wn * 32 + (lane % Epi::LPR) * 8);
       };
 #pragma unroll 1
-      for (int ha = 0; ha < (half ? 1 : 2); ++ha) {
+      for (int q = 0; q < 4; ++q) {
+        const int ha = q & 1, hb = q >> 1;
         if (ha == 0) {
-          dump(acc[0]);
-        } else {
-          __syncthreads();  // the first half has been read
-          dump(acc[1]);
+          if (hb && x.o.part) put_sums(0);
+          x.columns(n0 + hb * 128 + wn * 32);
+        } else if (half) {
+          continue;
         }
-        __syncthreads();
-        x.rows(smem, m0 + ha * 128, min(128, Mrows - m0 - ha * 128));
+        if (q == 0) dump(acc[0][0]);
+        else if (q == 1) dump(acc[1][0]);
+        else if (q == 2) dump(acc[0][1]);
+        else dump(acc[1][1]);
+        const int m = m0 + ha * 128 + wm * 64;
+        x.rows(block, m, Mrows - m);
       }
       if (x.o.part) {
+        put_sums(1);
         __syncthreads();
-        x.sums(smem);
+        add_sums<2 * Epi::RP>(table, 256, x.o.part + n0, min(256, Ncols - n0), (int)threadIdx.x);
       }
     } else {
     const float s = p.scale;
@@ -331,6 +340,7 @@ __device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds
     store_tile<256, 512, kPOutRow>(smem, rc, m0 * ldc_b + n0 * 2, ldc_b, min(half ? 128 : 256, Mrows - m0),
                                    min(256, Ncols - n0), p.c_vec != 0, (int)threadIdx.x);
     }
+    if constexpr (EP::on) break;  // one work item a call
     if (tb + nwg < total) __syncthreads();  // the next tile's copies overwrite the output rows
   }
 }

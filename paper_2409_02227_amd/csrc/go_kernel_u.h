@@ -142,7 +142,7 @@ template <int DT, int BM, int BN, int WM, int WN, int STAGES> struct UCfg {
 // The tiles of one member: work items lwg, lwg + nwg, ... of p, by the whole
 // workgroup, in the LDS at smem (UCfg::LDS bytes).  ANY: both ways, else
 // copies only.  SPLIT: members may be split along K.  EP: where the results
-// go (NoEpi: to C, scaled and rounded).
+// go (NoEpi: to C, scaled and rounded); with an epilogue, work item lwg alone.
 template <int DT, int TA, int TB, int BM, int BN, int WM, int WN, int STAGES, bool ANY, bool SPLIT, bool JOINT,
           class EP = NoEpi>
 __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds_u8* smem, EP ep = EP()) {
@@ -406,6 +406,7 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
               }
             }
         }
+        if constexpr (EP::on) break;
         __syncthreads();  // every wave is done with the stages before the next item refills them
         continue;
       }
@@ -413,29 +414,31 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
 
     // accumulator r of lane l is n = 4*(l/16) + r, m = l%16 of its block
     __syncthreads();  // every wave has read its last fragments
-    if constexpr (EP::on) {  // fp32 rows, up to 64 at a time
-      typedef EpiTile<DT, BN, C::NW * 64> Epi;
-      constexpr int HR = BM < 64 ? BM : 64;
-      static_assert(HR * Epi::PITCH <= C::LDS && C::NW * 64 * 32 <= C::LDS, "the rows and the sums fit in the ring");
-      Epi x(ep(item, tm), n0, tid);
+    if constexpr (EP::on) {
+      constexpr int R = WTM < 32 ? WTM : 32;
+      typedef EpiWave<DT, R, WTN, EP::ahead> Epi;
+      static_assert(C::NW * Epi::BYTES <= C::LDS && WM * Epi::RP * BN * 4 <= C::LDS, "blocks and sums fit in the ring");
+      Epi x(ep(item, tm), lane);
+      lds_u8* block = smem + wave * Epi::BYTES;
+      x.columns(n0 + wn * WTN);
 #pragma unroll 1
-      for (int h = 0; h < BM / HR && m0 + h * HR < Mrows; ++h) {
-        if (h) __syncthreads();  // the rows before have been read
+      for (int h = 0; h < WTM / R; ++h) {
 #pragma unroll
         for (int i = 0; i < C::FM; ++i) {
-          const int r = wm * WTM + i * 16 - h * HR;
-          if (r < 0 || r >= HR) continue;
+          if (i / (R / 16) != h) continue;
 #pragma unroll
           for (int j = 0; j < C::FN; ++j)
-            *(__attribute__((address_space(3))) f32x4*)(smem + (r + (lane & 15)) * Epi::PITCH +
-                                                        (wn * WTN + j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i];
+            *(__attribute__((address_space(3))) f32x4*)(block + ((i % (R / 16)) * 16 + (lane & 15)) * Epi::PITCH +
+                                                        (j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i];
         }
-        __syncthreads();
-        x.rows(smem, m0 + h * HR, min(HR, Mrows - m0 - h * HR));
+        const int m = m0 + wm * WTM + h * R;
+        x.rows(block, m, Mrows - m);
       }
       if (x.o.part) {
         __syncthreads();
-        x.sums(smem);
+        x.put_sums(smem, wm * Epi::RP + lane / Epi::LPR, BN, wn * WTN + (lane % Epi::LPR) * 8);
+        __syncthreads();
+        add_sums<WM * Epi::RP>(smem, BN, x.o.part + n0, min(BN, Ncols - n0), tid);
       }
     } else {
     const float s = p.scale;
@@ -472,6 +475,7 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
                                          min(BN, Ncols - n0), p.c_vec != 0, tid);
     }
     }
+    if constexpr (EP::on) break;  // one work item a call
     if (tb + nwg < total) __syncthreads();  // the next tile's copies overwrite the output rows
   }
 }

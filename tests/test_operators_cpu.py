@@ -296,7 +296,7 @@ def test_null_arguments(ctx):
 
 
 # ---- the kernels' code -------------------------------------------------------------
-@pytest.mark.parametrize("unit", [f"kernels_{f}_{dt}" for f in ("ep", "group") for dt in ("bf16", "f16", "fp8", "f32")])
+@pytest.mark.parametrize("unit", [f"kernels_{f}_{dt}" for f in ("ep", "ep1", "group") for dt in ("bf16", "f16", "fp8", "f32")])
 def test_wait_states_and_no_scratch(tmp_path, unit):
     """As test_copy_wait_states, for the kernels of epilogues and grouped products."""
     obj = os.path.join(waits.BUILD, unit + ".o")
