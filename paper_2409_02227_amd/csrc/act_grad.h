@@ -48,7 +48,7 @@ static __global__ void __launch_bounds__(256) group_sums(GroupSums s) {
     const GroupRows g = group_rows(s.offsets, s.groups, s.rows, e);
     count = min((g.count + s.bm - 1) / s.bm, max(s.max_slots - first, 0));
   }
-  column_sums(s.part + (int64_t)first * s.n, s.out + e * s.stride, s.n, count, col, lds);
+  column_sums(s.part + (int64_t)first * s.per * s.n, s.out + e * s.stride, s.n, count * s.per, col, lds);
 }
 
 // A workgroup: bm rows of a group x kActCols columns, a lane eight consecutive ones.

@@ -47,14 +47,14 @@ struct NoEpi {
 template <int AHEAD> struct MemberEpi {
   static constexpr bool on = true;
   static constexpr int ahead = AHEAD;
+  static constexpr int kAt = (sizeof(KLaunch) + alignof(KEpis) - 1) / alignof(KEpis) * alignof(KEpis);
   typedef const __attribute__((address_space(4))) uint8_t* Ptr;
   int gi;
   __device__ __forceinline__ EpiOut operator()(int item, int tile_row) const {
-    constexpr int at = (sizeof(KLaunch) + alignof(KEpis) - 1) / alignof(KEpis) * alignof(KEpis);
     Ptr args = (Ptr)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(args));
     const auto* a = (const __attribute__((address_space(4))) KArgs*)(args + offsetof(KLaunch, g)) + gi;
-    const auto* e = (const __attribute__((address_space(4))) KEpi*)(args + at) + gi;
+    const auto* e = (const __attribute__((address_space(4))) KEpi*)(args + kAt) + gi;
     EpiOut o;
     o.c = a->c + item * a->stride_c;
     o.c_bytes = a->c_bytes, o.ldc = (int)a->ldc, o.m = (int)a->m, o.n = (int)a->n;

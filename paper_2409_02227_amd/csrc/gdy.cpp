@@ -1352,25 +1352,46 @@ bool use_rows128(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int
   return rows128_wins(launch_cus(ctx, p, mode, p.stream_of[members[0]]), g, members);
 }
 
+// Whether a launch with epilogues whose members all run 128 x 128 tiles of an
+// untransposed A runs 64 x 128 ones: where the larger would not fill the CUs once
+// (bf16 with a bias: (512, 6144, 12288) nn 128 -> 108 us, (1024, 4096, 1024) nt 18.4 ->
+// 15.4; (2048, 4096, 4096) nt, two tiles a CU, 63 and 84).  Rows do not enter an element's sum.
+bool use_rows64(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int mode, const Members& members,
+                int joint) {
+  int64_t tiles = 0;
+  for (int i : members) {
+    if (is_add_variant(ctx, p.variant_of[i])) continue;
+    const Exec e = joint_exec(ctx, p.variant_of[i], g[i], joint);
+    if (joint != 1 || e.family != 1 || (e.code & 7) != 0 || g[i].trans_a || p.split_of[i] > 1 ||
+        ctx->variants[p.variant_of[i]].cap > 0)
+      return false;
+    tiles += (g[i].m + 127) / 128 * ((g[i].n + 127) / 128) * std::max(g[i].batch, 1);
+  }
+  return tiles <= launch_cus(ctx, p, mode, p.stream_of[members[0]]);
+}
+
 // Workgroup ranges of one dispatch: each GEMM gets its own grid (tiles, or
 // its cap x occupancy), every range but the last rounded up to a multiple
-// of 8 so each GEMM starts on XCD 0 (the extra workgroups find no tile).
+// of 8 so each GEMM starts on XCD 0 (the extra workgroups find no tile).  lower:
+// use_rows64 may apply.
 gdy_status build_launch(gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int mode,
                         const Members& members, int joint, const std::vector<int64_t>& ws_off,
-                        float* ws_base, int64_t ws_cap, KLaunch* L, int* grid, bool* split) {
+                        float* ws_base, int64_t ws_cap, KLaunch* L, int* grid, bool* split, bool lower = false) {
   // of an unplaced block the kernels read count, first, placed and g[0 .. count)
   L->count = members.size();
   L->placed = 0;
   *split = false;
   int64_t wg = 0;
   const bool rows128 = use_rows128(ctx, g, p, mode, members, joint);
+  const bool rows64 = lower && use_rows64(ctx, g, p, mode, members, joint);
   bool one_tile = true;  // every member runs the same tile
   int tile_m = 0, tile_n = 0;
   for (int u = 0; u < L->count; ++u) {
     const int i = members[u];
     const Variant& v = ctx->variants[p.variant_of[i]];
     const KernelDesc* d = ctx->kernels[v.kernel].d;
-    const Exec e = joint ? joint_exec(ctx, p.variant_of[i], g[i], joint) : exec_of(ctx, p.variant_of[i], g[i]);
+    Exec e = joint ? joint_exec(ctx, p.variant_of[i], g[i], joint) : exec_of(ctx, p.variant_of[i], g[i]);
+    if (rows64 && !d->ew) e.jbm = 64, e.code += 1;  // the 64 x 128 tile of its layout
     KArgs& a = L->g[u];
     a = make_args(ctx, p.variant_of[i], g[i]);
     if (!d->ew) {
@@ -1551,10 +1572,11 @@ const void* lone_epilogue_kernel(int dtype, int family, int code, bool copies) {
 }
 
 // Rows of partial column sums that an item of g may take: its tile rows, or those
-// of the split reduction.  Members of 256 x 256 kernels may run 128-row tiles.
+// of the split reduction.  Members of larger tiles may run 128- or 64-row ones.
 int64_t part_rows(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
   if (p.split_of[i] > 1) return (g.m + kEpiReduceRows - 1) / kEpiReduceRows;
-  const int bm = std::min(exec_of(ctx, p.variant_of[i], g).jbm, 128);
+  int bm = std::min(exec_of(ctx, p.variant_of[i], g).jbm, 128);
+  if (bm == 128) bm = 64;  // use_rows64
   return (g.m + bm - 1) / bm;
 }
 int64_t part_bytes(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
@@ -1972,7 +1994,8 @@ gdy_status launch_plan(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue* ep, 
       bool with_ep = false;
       for (int i : members) with_ep = with_ep || (ep && has_epilogue(ep[i]));
       const int joint = with_ep && !x.joint ? ex.family : x.joint;
-      st = build_launch(ctx, g, p, mode, members, joint, ws_off, ws_base, ws_cap, &launch, &grid, &split);
+      st = build_launch(ctx, g, p, mode, members, joint, ws_off, ws_base, ws_cap, &launch, &grid, &split,
+                        with_ep);
       if (st != GDY_OK) break;
       void* argv[] = {&launch};
       const int d = x.dispatch;

@@ -145,12 +145,14 @@ struct KGroup {
   int32_t lda, ldb, ldc;   // elements
   float scale;
   int32_t a_dma, b_dma, c_vec;
+  int32_t bm;              // over rows: rows of a tile
   int32_t max_slots;       // over rows: the most row tiles
+  int32_t xcd_cus;         // CUs of an XCD
   KEpi epi;                // over K: the residual only; strides between groups
 };
 
 // A kernel of grouped products: its tile and threads.  Tiles by index: 256 x 256,
-// 128 x 128, 64 x 128 (over K 64 x 64), and over rows 32 x 128 and 16 x 64.
+// 128 x 128, 64 x 128 (over K 64 x 64), and over rows 32 x 128 and 32 x 64.
 struct GroupKernel {
   const void* func;
   int bm, bn, threads;
@@ -166,14 +168,14 @@ struct BiasSums {
   int32_t n[kMaxFused], rows[kMaxFused];
 };
 
-// The partial sums of grouped rows: those of group e's row tiles of bm rows, to
-// out[e]; shared: of all groups, to out[0].
+// The partial sums of grouped rows: those of group e's row tiles of bm rows, `per` rows of
+// sums a tile, to out[e]; shared: of all groups, to out[0].
 struct GroupSums {
   const float* part;
   float* out;
   const int32_t* offsets;
   int64_t stride;
-  int32_t n, rows, groups, bm, max_slots, shared;
+  int32_t n, rows, groups, bm, max_slots, shared, per;
 };
 // dz = dy * f'(z), and partial column sums by row tile.
 struct KActGrad {

@@ -2,8 +2,7 @@
 // tiles of the joint kernels of go_kernel_u.h and go_kernel_p.h, so an element's
 // fp32 sum is that of the plain launch.  Members of one tile and layout run on a
 // kernel of their own; go_gemm_ep and go_gemm_p_ep run mixed ones, as the joint
-// kernels do: their size costs registers and scalars in lanes of vector registers,
-// MIXED_COST.
+// kernels do.
 #pragma once
 #include "go_kernel_u.h"
 

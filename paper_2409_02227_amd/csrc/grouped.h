@@ -158,24 +158,42 @@ template <int DT, int TA, int TB, int BM_, int BN_, int WM, int WN, int STAGES> 
 };
 
 // Over rows.  The hardware deals workgroup b to XCD b % 8; each XCD takes a
-// contiguous run of the tiles, so that a group's B is read by one or two L2s.
+// contiguous run of the tiles, so that a group's B is read by one or two L2s.  A CU
+// holds one 256 x 256 tile: where an XCD's last tiles would leave half of its CUs idle
+// they run as halves of 128 rows, on twice as many (8192 rows in 16 groups x 4096,
+// 80 tiles an XCD: 170 -> 162 us).  The halves have partial sums of their own, so
+// every 256-row tile has two rows of them.
 template <int DT, int TB, class T>
 __global__ void __launch_bounds__(T::NT) grouped_rows(KGroup g) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDS];
   constexpr int ES = ElemSize<DT>::v;
+  const int bm = T::BM == 256 ? g.bm : T::BM;  // the 256 x 256 kernel has 128-row tiles too
+  const bool two = T::BM == 256 && bm == 256;
   const int tn = (g.n + T::BN - 1) / T::BN;
-  const int total = total_slots(g.offsets, g.groups, g.rows, T::BM, g.max_slots) * tn;
+  const int total = total_slots(g.offsets, g.groups, g.rows, bm, g.max_slots) * tn;
   const int per = (total + kXcds - 1) / kXcds;
-  const int j = (int)blockIdx.x / kXcds, id = ((int)blockIdx.x & (kXcds - 1)) * per + j;
+  int j = (int)blockIdx.x / kXcds, half = -1;
+  if (two) {
+    const int rest = per % g.xcd_cus;
+    if (2 * rest <= g.xcd_cus && j >= per - rest) {
+      half = (j - (per - rest)) & 1;
+      j = per - rest + (j - (per - rest)) / 2;
+    }
+  }
+  const int id = ((int)blockIdx.x & (kXcds - 1)) * per + j;
   if (j >= per || id >= total) return;
   GroupSlot s;
-  if (!find_slot(g.offsets, g.groups, g.rows, T::BM, id / tn, s)) return;
+  if (!find_slot(g.offsets, g.groups, g.rows, bm, id / tn, s)) return;
   int ti, tj;
-  group_tile(id - s.first * tn, (s.count + T::BM - 1) / T::BM, tn, ti, tj);
-  const int m0 = ti * T::BM, n0 = tj * T::BN;
+  group_tile(id - s.first * tn, (s.count + bm - 1) / bm, tn, ti, tj);
+  const int m0 = ti * bm + (half > 0 ? 128 : 0), n0 = tj * T::BN;
   GroupEpi e;
   e.e = uniform(s.e), e.row = uniform(s.lo + m0), e.n0 = uniform(n0);
-  e.m = uniform(min(T::BM, s.count - m0)), e.n = uniform(min(T::BN, g.n - n0)), e.slot = uniform(s.first + ti);
+  e.m = uniform(min(half >= 0 ? 128 : bm, s.count - m0)), e.n = uniform(min(T::BN, g.n - n0));
+  e.slot = uniform(two ? 2 * (s.first + ti) + (half > 0) : s.first + ti);
+  if (two && g.epi.part && (half < 0 || e.m <= 0) && (int)threadIdx.x < e.n)  // the sums of no half
+    g.epi.part[(int64_t)(half < 0 ? e.slot + 1 : e.slot) * g.n + n0 + threadIdx.x] = 0.0f;
+  if (e.m <= 0) return;
   e.os = OutSize<DT>::v, e.over_k = false;
   const uint8_t* a = g.a + (int64_t)e.row * g.lda * ES;
   const uint8_t* b = g.b + e.e * g.stride_b + (TB == 1 ? (int64_t)e.n0 * g.ldb : (int64_t)e.n0) * ES;
@@ -219,7 +237,7 @@ template <int DT, int TB> GroupKernel rows_kernel(int tile) {
     case 1: return GDY_GROUP_ROWS(DT, TB, TileU<DT, 0, TB, 128, 128, 2, 2, 2>);
     case 2: return GDY_GROUP_ROWS(DT, TB, TileU<DT, 0, TB, 64, 128, 2, 2, 3>);
     case 3: return GDY_GROUP_ROWS(DT, TB, TileU<DT, 0, TB, 32, 128, 1, 4, 4>);
-    case 4: return GDY_GROUP_ROWS(DT, TB, TileU<DT, 0, TB, 16, 64, 1, 4, 2>);
+    case 4: return GDY_GROUP_ROWS(DT, TB, TileU<DT, 0, TB, 32, 64, 1, 4, 4>);
     default: return GroupKernel{nullptr, 0, 0, 0};
   }
 }

@@ -242,16 +242,56 @@ GroupKernel group_kernel_of(int dtype, int over_k, int tb, int tile) {
          : dtype == DT_FP8 ? group_fp8(over_k, tb, tile) : group_f32(over_k, tb, tile);
 }
 
-int group_tile_of(const gdy_ctx* ctx, const gdy_grouped& g, bool copies) {
-  const bool wide = copies && g.a_type != GDY_F32;
-  if (g.over == GDY_OVER_K) {
-    const int64_t tiles = (g.k + 255) / 256 * ((g.n + 255) / 256) * g.groups;
-    if (wide && tiles >= ctx->cus / 2) return 0;
-    return (g.k + 127) / 128 * ((g.n + 127) / 128) * g.groups >= ctx->cus / 2 ? 1 : 2;
+// What a tile of a grouped product over rows costs, in times of a 256 x 256 tile's
+// step of K (fp32: of as many multiply-adds): `share` of a CU where tiles fill the
+// GPU, `item` from its start to its end, `waves` where a CU holds one at a time.
+// Measured at K = 2048 and 4096 in bf16, 8 to 128 groups of 64 to 8192 rows in all:
+// 8192 rows in 16 groups x 4096 took 170, 198, 196, 228, 325 and 370 us on these
+// tiles, 512 rows in 4 groups x 1024 83, 59, 47, 32, 26 and 26.
+struct GroupTileCost {
+  int tile, bm, bn;
+  double share, item;
+  bool waves;
+};
+const GroupTileCost kGroupTiles[] = {
+    {0, 256, 256, 1.0, 1.0, true},     {0, 128, 256, 0.65, 0.65, true},   {1, 128, 128, 0.32, 0.57, false},
+    {2, 64, 128, 0.21, 0.38, false},   {3, 32, 128, 0.145, 0.31, false},  {4, 32, 64, 0.08, 0.30, false}};
+const GroupTileCost kGroupTilesF32[] = {
+    {1, 128, 128, 0.25, 0.27, false},  {2, 64, 128, 0.13, 0.15, false},   {3, 32, 128, 0.07, 0.09, false},
+    {4, 32, 64, 0.037, 0.06, false}};
+
+// The kernel and tile rows of a product over rows.  The groups' sizes are unknown
+// here: as exponentially distributed, E groups of T rows make E / (1 - exp(-bm E /
+// T)) tiles of bm rows (E where groups are small, T / bm + E / 2 where they are
+// large; the 83 tiles of 60 groups of 8192 rows by a power law, bm = 256, count as 71).
+const GroupTileCost& group_rows_tile(const gdy_ctx* ctx, const gdy_grouped& g, bool copies) {
+  const bool f32 = g.a_type == GDY_F32;
+  const GroupTileCost* list = f32 ? kGroupTilesF32 : kGroupTiles;
+  const int n = f32 ? (int)(sizeof kGroupTilesF32 / sizeof *list) : (int)(sizeof kGroupTiles / sizeof *list);
+  const double cus = ctx->cus, groups = (double)std::min<int64_t>(g.groups, g.rows), avg = (double)g.rows / groups;
+  const GroupTileCost* best = nullptr;
+  double best_t = 0;
+  for (int i = 0; i < n; ++i) {
+    const GroupTileCost& c = list[i];
+    if (c.tile == 0 && !copies) continue;
+    const double rows = groups <= 1 ? std::ceil((double)g.rows / c.bm) : groups / (1.0 - std::exp(-c.bm / avg));
+    const double tiles = rows * (double)((g.n + c.bn - 1) / c.bn);
+    double t;
+    if (c.waves) {  // a last wave of up to half the CUs runs as halves of 256-row tiles
+      const double full = std::floor(tiles / cus), rest = tiles / cus - full;
+      t = full * c.item + (rest == 0 ? 0.0 : c.bm == 256 && rest <= 0.5 ? 0.65 : c.item);
+    }
+    else t = tiles * c.share <= cus * c.item ? c.item : tiles * c.share / cus + 0.5 * c.item;
+    if (!best || t < best_t) best = &c, best_t = t;
   }
-  const int64_t avg = g.rows / g.groups;
-  if (wide && avg >= 192) return 0;
-  return avg >= 96 ? 1 : avg >= 48 ? 2 : avg >= 24 ? 3 : 4;
+  return *best;
+}
+
+// The kernel of a product over K.
+int group_k_tile(const gdy_ctx* ctx, const gdy_grouped& g, bool copies) {
+  auto tiles = [&](int64_t b) { return (g.k + b - 1) / b * ((g.n + b - 1) / b) * g.groups; };
+  if (copies && g.a_type != GDY_F32 && tiles(256) >= ctx->cus / 2) return 0;
+  return tiles(128) >= ctx->cus / 2 ? 1 : 2;
 }
 
 gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue* ep, hipStream_t hs) {
@@ -292,9 +332,14 @@ gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue
     return (uintptr_t)p % 8 == 0 && (ld * os) % 8 == 0 && (!over_k || g.groups == 1 || (stride * os) % 8 == 0);
   };
   a.c_vec = vec(g.c, g.ldc, g.stride_c);
-  const int tile = group_tile_of(ctx, g, a.a_dma && a.b_dma);
-  const GroupKernel kern = group_kernel_of(g.a_type, over_k, g.trans_b, tile);
-  a.max_slots = (int32_t)max_row_tiles(g.rows, g.groups, kern.bm);
+  const bool copies = a.a_dma && a.b_dma;
+  const GroupTileCost* rows_tile = over_k ? nullptr : &group_rows_tile(ctx, g, copies);
+  const GroupKernel kern =
+      group_kernel_of(g.a_type, over_k, g.trans_b, over_k ? group_k_tile(ctx, g, copies) : rows_tile->tile);
+  a.bm = over_k ? kern.bm : rows_tile->bm;
+  a.max_slots = (int32_t)max_row_tiles(g.rows, g.groups, a.bm);
+  a.xcd_cus = std::max(ctx->cus / kXcds, 1);
+  const int sums_per_tile = !over_k && a.bm == 256 ? 2 : 1;
   if (ep) {
     a.epi.bias = (const uint8_t*)ep->bias;
     a.epi.bias_f32 = ep->bias && ep->bias_type == GDY_F32;
@@ -310,7 +355,7 @@ gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue
     a.epi.grad = ep->grad;
   }
   if (bias_grad) {
-    const int64_t need = (int64_t)a.max_slots * g.n * 4;
+    const int64_t need = (int64_t)a.max_slots * sums_per_tile * g.n * 4;
     if (need > kSplitWsBytes)
       return fail(ctx, GDY_ERR_UNSUPPORTED, "grouped: bias_grad needs %lld bytes of workspace, %lld are there",
                   (long long)need, (long long)kSplitWsBytes);
@@ -318,12 +363,12 @@ gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue
   }
   const int64_t tn = (g.n + kern.bn - 1) / kern.bn;
   const int64_t grid = over_k ? (((m + kern.bm - 1) / kern.bm * tn + kXcds - 1) / kXcds) * kXcds * g.groups
-                              : ((int64_t)a.max_slots * tn + kXcds - 1) / kXcds * kXcds;
+                              : (((int64_t)a.max_slots * tn + kXcds - 1) / kXcds + a.xcd_cus / 2) * kXcds;
   void* argv[] = {&a};
   HIP_TRY(ctx, hipExtLaunchKernel(kern.func, dim3((unsigned)grid), dim3(kern.threads), argv, 0, hs, nullptr, nullptr, 0));
   if (bias_grad) {
-    GroupSums s = {ctx->split_ws, bias_grad, g.offsets, ep->stride_bias_grad, a.n, a.rows, a.groups, kern.bm,
-                   a.max_slots, shared ? 1 : 0};
+    GroupSums s = {ctx->split_ws, bias_grad, g.offsets, ep->stride_bias_grad, a.n, a.rows, a.groups, a.bm,
+                   a.max_slots, shared ? 1 : 0, sums_per_tile};
     void* sargv[] = {&s};
     const int64_t blocks = (g.n + 63) / 64;
     HIP_TRY(ctx, hipExtLaunchKernel(group_sum_kernel(), dim3((unsigned)(blocks * (shared ? 1 : g.groups))), dim3(256),
@@ -431,7 +476,7 @@ gdy_status launch_act_grad(gdy_ctx* ctx, const gdy_act_grad& g, hipStream_t hs) 
     HIP_TRY(ctx, launch_bias_sums(&s, hs, nullptr));
   } else {
     GroupSums s = {a.part, g.bias_grad, g.offsets, g.stride_bias_grad, a.n, a.rows, groups, a.bm, a.max_slots,
-                   shared ? 1 : 0};
+                   shared ? 1 : 0, 1};
     void* sargv[] = {&s};
     HIP_TRY(ctx, hipExtLaunchKernel(group_sum_kernel(), dim3((unsigned)((g.n + 63) / 64 * (shared ? 1 : groups))), dim3(256),
                                     sargv, 0, hs, nullptr, nullptr, 0));
