@@ -1352,38 +1352,49 @@ bool use_rows128(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int
   return rows128_wins(launch_cus(ctx, p, mode, p.stream_of[members[0]]), g, members);
 }
 
-// Whether a launch with epilogues whose members all run 128 x 128 tiles of an
-// untransposed A runs 64 x 128 ones: where the larger would not fill the CUs once
-// (bf16 with a bias: (512, 6144, 12288) nn 128 -> 108 us, (1024, 4096, 1024) nt 18.4 ->
-// 15.4; (2048, 4096, 4096) nt, two tiles a CU, 63 and 84).  Rows do not enter an element's sum.
-bool use_rows64(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int mode, const Members& members,
-                int joint) {
+// The tile of a launch with epilogues whose members all run 128 x 128 tiles, uncapped,
+// and leave CUs without one: 64 x 128 (twice the workgroups, two a CU; unsplit
+// members), or for more than kDeepKTiles K tiles (kDeepRunTiles a run), where both
+// operands take copies, a ring of four stages of the same tile (0: as it is).  bf16 with weights from HBM, 128 x 128 tiles
+// of four stages against 64 x 128 ones of three: (1024, 4096, 1024) nt 19.6 and 17.1 us,
+// (512, 6144, 4096) nn 44.8 and 43.6, (512, 6144, 6144) 65 and 86, (512, 6144, 12288) 124 and
+// 161.  Neither changes an element's sum.
+const int kDeepKTiles = 64, kDeepRunTiles = 32;
+int few_tiles(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int mode, const Members& members,
+              int joint) {
   int64_t tiles = 0;
+  bool deep = true, first = true, low = true;
+  int code = 0;
   for (int i : members) {
     if (is_add_variant(ctx, p.variant_of[i])) continue;
     const Exec e = joint_exec(ctx, p.variant_of[i], g[i], joint);
-    if (joint != 1 || e.family != 1 || (e.code & 7) != 0 || g[i].trans_a || p.split_of[i] > 1 ||
-        ctx->variants[p.variant_of[i]].cap > 0)
-      return false;
-    tiles += (g[i].m + 127) / 128 * ((g[i].n + 127) / 128) * std::max(g[i].batch, 1);
+    if (joint != 1 || e.family != 1 || (e.code & 7) != 0 || ctx->variants[p.variant_of[i]].cap > 0) return 0;
+    const int split = std::max(p.split_of[i], 1);
+    deep = deep && a_copies(g[i]) && b_copies(g[i]) && (first || e.code == code) &&
+           g[i].k * elem_size(g[i].a_type) / split > (split > 1 ? kDeepRunTiles : kDeepKTiles) * kTileKBytes;
+    low = low && !g[i].trans_a && split == 1;
+    first = false;
+    code = e.code;
+    tiles += (g[i].m + 127) / 128 * ((g[i].n + 127) / 128) * std::max(g[i].batch, 1) * split;
   }
-  return tiles <= launch_cus(ctx, p, mode, p.stream_of[members[0]]);
+  if (tiles > launch_cus(ctx, p, mode, p.stream_of[members[0]])) return 0;
+  return deep ? 5 : low ? 1 : 0;
 }
 
 // Workgroup ranges of one dispatch: each GEMM gets its own grid (tiles, or
 // its cap x occupancy), every range but the last rounded up to a multiple
-// of 8 so each GEMM starts on XCD 0 (the extra workgroups find no tile).  lower:
-// use_rows64 may apply.
+// of 8 so each GEMM starts on XCD 0 (the extra workgroups find no tile).  epilogues:
+// for their kernels.
 gdy_status build_launch(gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int mode,
                         const Members& members, int joint, const std::vector<int64_t>& ws_off,
-                        float* ws_base, int64_t ws_cap, KLaunch* L, int* grid, bool* split, bool lower = false) {
+                        float* ws_base, int64_t ws_cap, KLaunch* L, int* grid, bool* split, bool epilogues = false) {
   // of an unplaced block the kernels read count, first, placed and g[0 .. count)
   L->count = members.size();
   L->placed = 0;
   *split = false;
   int64_t wg = 0;
   const bool rows128 = use_rows128(ctx, g, p, mode, members, joint);
-  const bool rows64 = lower && use_rows64(ctx, g, p, mode, members, joint);
+  const int few = epilogues ? few_tiles(ctx, g, p, mode, members, joint) : 0;
   bool one_tile = true;  // every member runs the same tile
   int tile_m = 0, tile_n = 0;
   for (int u = 0; u < L->count; ++u) {
@@ -1391,7 +1402,12 @@ gdy_status build_launch(gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, in
     const Variant& v = ctx->variants[p.variant_of[i]];
     const KernelDesc* d = ctx->kernels[v.kernel].d;
     Exec e = joint ? joint_exec(ctx, p.variant_of[i], g[i], joint) : exec_of(ctx, p.variant_of[i], g[i]);
-    if (rows64 && !d->ew) e.jbm = 64, e.code += 1;  // the 64 x 128 tile of its layout
+    if (few && !d->ew) {
+      e.code += few;
+      if (few == 1) e.jbm = 64;
+    } else if (epilogues && joint == 1 && !d->ew && (e.code & 7) == 4) {
+      e.jbm = 32;  // 16-row tiles: 32 rows and four stages there
+    }
     KArgs& a = L->g[u];
     a = make_args(ctx, p.variant_of[i], g[i]);
     if (!d->ew) {
@@ -1576,7 +1592,7 @@ const void* lone_epilogue_kernel(int dtype, int family, int code, bool copies) {
 int64_t part_rows(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
   if (p.split_of[i] > 1) return (g.m + kEpiReduceRows - 1) / kEpiReduceRows;
   int bm = std::min(exec_of(ctx, p.variant_of[i], g).jbm, 128);
-  if (bm == 128) bm = 64;  // use_rows64
+  if (bm == 128) bm = 64;  // few_tiles
   return (g.m + bm - 1) / bm;
 }
 int64_t part_bytes(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
@@ -1885,7 +1901,8 @@ gdy_status launch_epilogues(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue*
       copies = copies && launch.g[u].a_dma && launch.g[u].b_dma;
     }
     epis.e[u] = make_epi(g[i], ep[i], launch.g[u], part_off[i] >= 0 ? ws_base + part_off[i] / 4 : nullptr);
-    any_sums = any_sums || ep[i].bias_grad;
+    if (ep[i].bias_grad && epis.e[u].part_rows == 1 && g[i].batch <= 1) epis.e[u].part = ep[i].bias_grad;
+    else any_sums = any_sums || ep[i].bias_grad;
   }
   void* argv[] = {(void*)&launch, &epis};
   const void* func = one_code ? lone_epilogue_kernel(dtype, family, code, copies) : epilogue_kernel(dtype, family);
@@ -1913,7 +1930,7 @@ gdy_status launch_epilogues(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue*
   if (e == hipSuccess && any_sums) {
     for (int u = 0; u < launch.count; ++u) {
       const int i = members[u];
-      if (!ep[i].bias_grad) continue;
+      if (!ep[i].bias_grad || epis.e[u].part == ep[i].bias_grad) continue;  // one tile row is the sum
       const int items = std::max(g[i].batch, 1);
       const bool shared = items > 1 && ep[i].stride_bias_grad == 0;
       add_bias_sum(&sums, epis.e[u].part, ep[i].bias_grad, (int)g[i].n,

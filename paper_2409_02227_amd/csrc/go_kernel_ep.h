@@ -106,15 +106,16 @@ __global__ void __launch_bounds__(WM * WN * 64) go_gemm_ep1(KLaunch L, KEpis) {
 // Members of joint code `code`; copies: both operands of all of them take copies.
 template <int DT, int TA, int TB, int BM, int BN, int WM, int WN, int STAGES>
 const void* ep1_kernel(bool copies) {
-  if constexpr (BM >= 32)
-    if (copies) return reinterpret_cast<const void*>(&go_gemm_ep1<DT, TA, TB, BM, BN, WM, WN, STAGES, false>);
+  if (copies)
+    return reinterpret_cast<const void*>(&go_gemm_ep1<DT, TA, TB, BM, BN, WM, WN, STAGES, false>);
   return reinterpret_cast<const void*>(&go_gemm_ep1<DT, TA, TB, BM, BN, WM, WN, STAGES, true>);
 }
 template <int DT, int TA, int TB> const void* ep1_tile(int tile, bool copies) {
   switch (tile) {
     case 0: return ep1_kernel<DT, TA, TB, 128, 128, 2, 2, 2>(copies);
     case 2: return ep1_kernel<DT, TA, TB, 64, 64, 2, 2, 4>(copies);
-    case 4: return ep1_kernel<DT, TA, TB, 16, 64, 1, 4, 2>(copies);
+    case 4: return ep1_kernel<DT, TA, TB, 32, 64, 1, 4, 4>(copies);
+    case 5: return reinterpret_cast<const void*>(&go_gemm_ep1<DT, TA, TB, 128, 128, 2, 2, 4, false>);
     default:  // as joint_tiles
       if constexpr (TA == 0)
         return tile == 1 ? ep1_kernel<DT, TA, TB, 64, 128, 2, 2, 3>(copies) : ep1_kernel<DT, TA, TB, 32, 128, 1, 4, 4>(copies);

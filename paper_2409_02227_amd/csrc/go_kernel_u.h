@@ -87,7 +87,13 @@ template <int ES, bool KC, int ROWS, int NW, bool SPILLS> struct Operand {
       copy16_to_lds<SPILLS>(d, dst + (wave + NW * j) * 1024, o);
     }
   }
-  __device__ __forceinline__ void load(int kt, int wave) {
+  // Tile kt's chunks in registers, as loaded
+  struct Held {
+    u32x4 lo[N];
+    unsigned hi[N];
+  };
+  __device__ __forceinline__ void load(int kt, int wave) { load(kt, wave, lo, hi); }
+  __device__ __forceinline__ void load(int kt, int wave, u32x4 (&lo)[N], unsigned (&hi)[N]) const {
     if (!ALL && wave >= BLOCKS) return;
     const Rsrc r = make_rsrc(base + (int64_t)kt * step, bytes - kt * step);
 #pragma unroll
@@ -99,6 +105,10 @@ template <int ES, bool KC, int ROWS, int NW, bool SPILLS> struct Operand {
   }
   // K: elements of the run
   __device__ __forceinline__ void store(int kt, int K, lds_u8* dst, int wave, int lane) const {
+    store(kt, K, dst, wave, lane, lo, hi);
+  }
+  __device__ __forceinline__ void store(int kt, int K, lds_u8* dst, int wave, int lane, const u32x4 (&lo)[N],
+                                        const unsigned (&hi)[N]) const {
     if (!ALL && wave >= BLOCKS) return;
     const int left = K - kt * BK;  // elements of K from this tile on
 #pragma unroll
@@ -294,7 +304,41 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
       ob.copy(kt, K * C::ES, st + C::A_BYTES, wave);
     };
 
-    if (nk > 0) {
+    // Tiles that the register way of a kernel with epilogues holds in registers: HBM
+    // answers after 1.7 us, several times what a tile's arithmetic takes, so a tile is
+    // loaded that many before it is computed.  128 x 128 tiles have no registers left.
+    constexpr int HELD = !EP::on || BM * BN > 64 * 128 ? 0 : BM * BN > 64 * 64 || BN > 64 ? 2 : 3;
+    if (ANY && HELD > 0 && nk > 0 && !(acopy && bcopy)) {
+      if constexpr (ANY && HELD > 0) {
+        typename OpA::Held ha[HELD];
+        typename OpB::Held hb[HELD];
+        auto load = [&](int kt, int d) {
+          oa.load(kt, wave, ha[d].lo, ha[d].hi);
+          ob.load(kt, wave, hb[d].lo, hb[d].hi);
+        };
+        auto store = [&](int kt, int d) {
+          lds_u8* st = smem + (kt & 1) * C::STAGE;
+          oa.store(kt, K, st, wave, lane, ha[d].lo, ha[d].hi);
+          ob.store(kt, K, st + C::A_BYTES, wave, lane, hb[d].lo, hb[d].hi);
+          if (kt + HELD < nk) load(kt + HELD, d);
+        };
+#pragma unroll
+        for (int d = 0; d < HELD; ++d)
+          if (d < nk) load(d, d);
+        store(0, 0);
+        for (int k0 = 0; k0 < nk; k0 += HELD) {
+#pragma unroll
+          for (int d = 0; d < HELD; ++d) {
+            const int kt = k0 + d;
+            if (kt >= nk) break;
+            sync();
+            compute(smem + (kt & 1) * C::STAGE, [&]() {
+              if (kt + 1 < nk) store(kt + 1, (d + 1) % HELD);
+            });
+          }
+        }
+      }
+    } else if (nk > 0) {
       if (ANY && (STAGES == 2 || !acopy || !bcopy)) {
         // tile kt to its stage (register way: the values loaded before), and
         // the loads of the tile after it
@@ -517,7 +561,10 @@ __device__ __forceinline__ void joint_tiles(const KArgs& p, int lwg, int nwg, ld
   switch (p.code & 7) {
     case 0: u_tiles<DT, TA, TB, 128, 128, 2, 2, 2, true, true, true, EP>(p, lwg, nwg, smem, ep); break;
     case 2: u_tiles<DT, TA, TB, 64, 64, 2, 2, 4, true, true, true, EP>(p, lwg, nwg, smem, ep); break;
-    case 4: u_tiles<DT, TA, TB, 16, 64, 1, 4, 2, true, true, true, EP>(p, lwg, nwg, smem, ep); break;
+    case 4:
+      if constexpr (EP::on) u_tiles<DT, TA, TB, 32, 64, 1, 4, 4, true, true, true, EP>(p, lwg, nwg, smem, ep);
+      else u_tiles<DT, TA, TB, 16, 64, 1, 4, 2, true, true, true, EP>(p, lwg, nwg, smem, ep);
+      break;
     default:  // the catalogue has these for an untransposed A only
       if constexpr (TA == 0) {
         if ((p.code & 7) == 1) u_tiles<DT, TA, TB, 64, 128, 2, 2, 3, true, true, true, EP>(p, lwg, nwg, smem, ep);
