@@ -20,7 +20,7 @@ SOURCES = ["kernels_joint_bf16.hip", "kernels_joint_f16.hip", "kernels_joint_fp8
            "kernels_group_bf16.hip", "kernels_group_f16.hip", "kernels_group_fp8.hip", "kernels_group_f32.hip",
            "kernels_d_bf16.hip", "kernels_d_f16.hip", "kernels_d_fp8.hip",
            "kernels_bf16.hip", "kernels_f16.hip", "kernels_fp8.hip", "kernels_f32.hip", "kernels_ew.hip",
-           "kernels_act.hip", "gdy.cpp"]
+           "kernels_act.hip", "kernels_skinny.hip", "gdy.cpp"]
 ARCH = "gfx950"
 # -packed-fp32-ops: keep hipcc from forming packed fp32 ALU ops by itself.
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

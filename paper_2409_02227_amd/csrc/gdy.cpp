@@ -1587,6 +1587,17 @@ const void* lone_epilogue_kernel(int dtype, int family, int code, bool copies) {
          : dtype == DT_FP8 ? ep_lone_fp8(family, code, copies) : ep_lone_f32(family, code, copies);
 }
 
+// Whether a GEMM with an epilogue runs on the kernel of few rows (skinny.h: K in at
+// most two rounds of its loads), alone and beside others, whatever kernel the plan
+// names.
+bool skinny(const gdy_gemm& g, const gdy_epilogue& e) {
+  const int es = elem_size(g.a_type);
+  const int64_t round = 8 * skinny_kstep(es) * skinny_ahead(es, g.trans_b);
+  if (g.k * es > 2 * round) return false;
+  return g.op == GDY_OP_GEMM && g.m <= kSkinnyRows && !g.trans_a && g.k > 0 && has_epilogue(e) && a_copies(g) &&
+         b_copies(g) && skinny_ep(g.a_type, g.trans_b);
+}
+
 // Rows of partial column sums that an item of g may take: its tile rows, or those
 // of the split reduction.  Members of larger tiles may run 128- or 64-row ones.
 int64_t part_rows(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
@@ -1883,8 +1894,31 @@ void plan_units(const gdy_ctx* ctx, const gdy_gemm* g, gdy_plan_t* p, int mode, 
 void add_bias_sum(BiasSums* s, const float* part, float* out, int n, int rows, int items, int64_t stride);
 hipError_t launch_bias_sums(BiasSums* s, hipStream_t hs, hipEvent_t stop);
 
+// Launch block of members of few rows of one layout: a workgroup a column tile.
+void build_skinny(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, const Members& members, KLaunch* L,
+                  int* grid) {
+  L->count = members.size();
+  L->placed = 0;
+  int64_t wg = 0;
+  for (int u = 0; u < L->count; ++u) {
+    const gdy_gemm& x = g[members[u]];
+    KArgs& a = L->g[u];
+    a = make_args(ctx, p.variant_of[members[u]], x);
+    if (x.op == GDY_OP_GEMM) {  // (adds ride along on their own tiles)
+      const int cols = skinny_cols(x.trans_b);
+      a.tiles_m = 1;
+      a.tiles_n = (int32_t)((x.n + cols - 1) / cols);
+    }
+    L->first[u] = (int32_t)wg;
+    wg += (int64_t)a.tiles_m * a.tiles_n * a.batch;
+  }
+  L->first[L->count] = (int32_t)wg;
+  *grid = (int)wg;
+}
+
 // The epilogue launch of a unit: its members on the epilogue kernel of their
-// family, the reduction of the split ones, and the sums of the bias gradients.
+// family (0: the kernel of few rows), the reduction of the split ones, and the sums
+// of the bias gradients.
 gdy_status launch_epilogues(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue* ep, const Members& members,
                             int family, int dtype, const KLaunch& launch, int grid, bool split, float* ws_base,
                             const std::vector<int64_t>& part_off, hipStream_t hs, hipEvent_t start, hipEvent_t stop) {
@@ -1905,7 +1939,9 @@ gdy_status launch_epilogues(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue*
     else any_sums = any_sums || ep[i].bias_grad;
   }
   void* argv[] = {(void*)&launch, &epis};
-  const void* func = one_code ? lone_epilogue_kernel(dtype, family, code, copies) : epilogue_kernel(dtype, family);
+  const void* func = family == 0 ? skinny_ep(dtype, g[members[0]].trans_b)
+                     : one_code  ? lone_epilogue_kernel(dtype, family, code, copies)
+                                 : epilogue_kernel(dtype, family);
   hipError_t e = hipExtLaunchKernel(func, dim3(grid), dim3(family == 1 ? 256 : 512), argv, 0,
                                     hs, start, !split && !any_sums ? stop : nullptr, 0);
   if (e == hipSuccess && split) {
@@ -2001,45 +2037,77 @@ gdy_status launch_plan(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogue* ep, 
           i0 = i;
           break;
         }
-      const int vid = p.variant_of[i0];
-      const Exec ex = exec_of(ctx, vid, g[i0]);
       KLaunch launch;
       int grid = 0;
       bool split = false;
       // members with epilogues run on the epilogue kernel of their family, in the
-      // family's tiles
-      bool with_ep = false;
-      for (int i : members) with_ep = with_ep || (ep && has_epilogue(ep[i]));
-      const int joint = with_ep && !x.joint ? ex.family : x.joint;
-      st = build_launch(ctx, g, p, mode, members, joint, ws_off, ws_base, ws_cap, &launch, &grid, &split,
-                        with_ep);
-      if (st != GDY_OK) break;
-      void* argv[] = {&launch};
+      // family's tiles, those of few rows on launches of their own
+      bool with_ep = false, skinny_ran = false;
+      std::vector<int> few[2], rest;  // by layout of B
       const int d = x.dispatch;
-      if (with_ep) {
-        st = launch_epilogues(ctx, g, ep, members, joint, g[i0].a_type, launch, grid, split, ws_base, part_off,
-                              p.stream_of[i0] >= 0 ? stream_at(p.stream_of[i0]) : origin, ts ? ts->start[d] : nullptr,
-                              ts ? ts->stop[d] : nullptr);
+      hipStream_t hs = p.stream_of[i0] >= 0 ? stream_at(p.stream_of[i0]) : origin;
+      hipEvent_t start = ts ? ts->start[d] : nullptr, stop = ts ? ts->stop[d] : nullptr;
+      if (ep) {
+        bool gemm = false;
+        for (int i : members) {
+          if (skinny(g[i], ep[i])) {
+            few[g[i].trans_b].push_back(i);
+            continue;
+          }
+          rest.push_back(i);
+          gemm = gemm || g[i].op == GDY_OP_GEMM;
+        }
+        if (rest.size() < (size_t)members.size() && !rest.empty() && !gemm) {  // adds ride along
+          std::vector<int>& with = few[0].empty() ? few[1] : few[0];
+          with.insert(with.end(), rest.begin(), rest.end());
+          rest.clear();
+        }
+        for (int tb = 0; tb < 2 && st == GDY_OK; ++tb) {
+          if (few[tb].empty()) continue;
+          const bool last = rest.empty() && (tb == 1 || few[1].empty());
+          build_skinny(ctx, g, p, few[tb], &launch, &grid);
+          st = launch_epilogues(ctx, g, ep, few[tb], 0, g[i0].a_type, launch, grid, false, ws_base, part_off, hs, start,
+                                last ? stop : nullptr);
+          start = nullptr;
+          skinny_ran = true;
+        }
         if (st != GDY_OK) break;
+        for (int i : rest) with_ep = with_ep || has_epilogue(ep[i]);
         if (ts) {
           ts->launched[d] = 1;
           for (int i : members) ts->dispatch_of[i] = d;
         }
+        if (rest.empty()) continue;
+      }
+      const Members run = ep ? Members(rest) : members;
+      if (skinny_ran)
+        for (int i : run)  // the first GEMM of what is left
+          if (!is_add_variant(ctx, p.variant_of[i])) {
+            i0 = i;
+            break;
+          }
+      const int vid = p.variant_of[i0];
+      const Exec ex = exec_of(ctx, vid, g[i0]);
+      const int joint = with_ep && !x.joint ? ex.family : x.joint;
+      st = build_launch(ctx, g, p, mode, run, joint, ws_off, ws_base, ws_cap, &launch, &grid, &split, with_ep);
+      if (st != GDY_OK) break;
+      void* argv[] = {&launch};
+      if (with_ep) {
+        st = launch_epilogues(ctx, g, ep, run, joint, g[i0].a_type, launch, grid, split, ws_base, part_off, hs, start,
+                              stop);
+        if (st != GDY_OK) break;
         continue;
       }
       const void* func = x.joint ? joint_kernel(g[i0].a_type, x.joint) : split ? ex.func_split : ex.func;
       const int waves = !x.joint ? ex.waves : x.joint == 1 ? 4 : 8;
-      hipStream_t hs = p.stream_of[i0] >= 0 ? stream_at(p.stream_of[i0]) : origin;
-      hipError_t e = hipExtLaunchKernel(func, dim3(grid), dim3(waves * 64), argv, 0, hs,
-                                        ts ? ts->start[d] : nullptr, ts && !split ? ts->stop[d] : nullptr, 0);
+      hipError_t e = hipExtLaunchKernel(func, dim3(grid), dim3(waves * 64), argv, 0, hs, start, split ? nullptr : stop, 0);
       if (e == hipSuccess && split) {
         // the split members' planes summed into C, on the same stream
         KLaunch red;
         int rgrid = 0;
-        build_reduce(ctx, g, p, members, launch, &red, &rgrid);
+        build_reduce(ctx, g, p, run, launch, &red, &rgrid);
         void* rargv[] = {&red};
-        e = hipExtLaunchKernel(split_reduce_kernel(g[i0].c_type), dim3(rgrid), dim3(256), rargv, 0, hs, nullptr,
-                               ts ? ts->stop[d] : nullptr, 0);
+        e = hipExtLaunchKernel(split_reduce_kernel(g[i0].c_type), dim3(rgrid), dim3(256), rargv, 0, hs, nullptr, stop, 0);
       }
       if (e != hipSuccess) {
         st = fail(ctx, GDY_ERR_HIP, "launch of %s (%d GEMMs, first %d) failed: %s",

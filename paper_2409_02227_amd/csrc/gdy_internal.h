@@ -235,6 +235,13 @@ const void* ep_lone_bf16(int family, int code, bool copies);
 const void* ep_lone_f16(int family, int code, bool copies);
 const void* ep_lone_fp8(int family, int code, bool copies);
 const void* ep_lone_f32(int family, int code, bool copies);
+// GEMMs of at most kSkinnyRows rows, by type and transposed B (null: none); the columns
+// of a workgroup, and the K bytes that its eight waves have in flight at a time.
+constexpr int kSkinnyRows = 16;
+const void* skinny_ep(int dt, int tb);
+constexpr int skinny_cols(int tb) { return tb ? 16 : 64; }
+constexpr int skinny_kstep(int es) { return es == 1 ? 128 : 64; }
+constexpr int skinny_ahead(int es, int tb) { return tb && es != 1 ? 8 : 4; }
 GroupKernel group_bf16(int over_k, int tb, int tile);
 GroupKernel group_f16(int over_k, int tb, int tile);
 GroupKernel group_fp8(int over_k, int tb, int tile);

@@ -1,0 +1,3 @@
+// bf16 GEMMs with epilogues: launches of one tile and layout.
+#include "go_kernel_ep.h"
+const void* gdy::ep_lone_bf16(int family, int code, bool copies) { return ep_lone<DT_BF16>(family, code, copies); }

@@ -1,0 +1,3 @@
+// f16 GEMMs with epilogues: launches of one tile and layout.
+#include "go_kernel_ep.h"
+const void* gdy::ep_lone_f16(int family, int code, bool copies) { return ep_lone<DT_F16>(family, code, copies); }

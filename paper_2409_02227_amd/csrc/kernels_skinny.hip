@@ -1,0 +1,10 @@
+// GEMMs of at most 16 rows with epilogues.
+#include "skinny.h"
+const void* gdy::skinny_ep(int dt, int tb) {
+  switch (dt) {
+    case DT_BF16: return skinny_kernel<DT_BF16>(tb);
+    case DT_F16: return skinny_kernel<DT_F16>(tb);
+    case DT_FP8: return skinny_kernel<DT_FP8>(tb);
+    default: return skinny_kernel<DT_F32>(tb);
+  }
+}

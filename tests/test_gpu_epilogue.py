@@ -153,6 +153,42 @@ def test_every_tile_by_name(ctx, variant):
         run(ctx, [c], mode="forced")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "fp8", "f32"])
+@pytest.mark.parametrize("m,n,k", [(1, 64, 64), (1, 2048, 2048), (2, 72, 136), (5, 200, 1000), (15, 24, 8192),
+                                   (16, 136, 520), (16, 16, 16), (16, 1000, 24)])
+def test_few_rows(ctx, dtype, m, n, k):
+    """The kernel of at most 16 rows: sizes below a wave's K step and not multiples of
+    it, one column block and many, batches, padded and aligned pitches."""
+    if dtype == "fp8":
+        k, n = (k + 15) // 16 * 16, (n + 15) // 16 * 16
+    for q, layout in enumerate(("nn", "nt")):
+        run(ctx, [Case(dtype, m, n, k, layout, ACTS[(q + m) % 5], bias="f32", residual=True, aux=True, sums="all",
+                       pad=(0, 16)[q]),
+                  Case(dtype, m, n, k, layout, ACTS[(q + n) % 5], grad=True, sums="all", seed=1),
+                  Case(dtype, m, n, k, layout, "silu", bias="own", sums=("items", "all")[q], items=3, bias_items=q == 0),
+                  Case(dtype, m, n, k, layout, seed=2)])
+
+
+def test_few_rows_give_the_same_bits_alone_and_beside_others(ctx):
+    gen = torch.Generator().manual_seed(9)
+    one = Case("bf16", 3, 520, 2048, "nt", "silu", bias="f32", sums="all")
+    run(ctx, [one])
+    ref = one.c.clone(), one.sums.clone()
+    x, y = operand(gen, 64, 128, "bf16"), operand(gen, 64, 128, "bf16")
+    for others in ([], [Case("bf16", 300, 520, 512, "nt", "gelu", grad=True, sums="all")],
+                   [Case("bf16", 2, 64, 512, "nn", "relu", bias="own"), Case("bf16", 700, 520, 512, "nn")]):
+        for add in ([], [gdy.Add(x, y, torch.empty_like(x)), gdy.Add(x.float(), y.float(), torch.empty(64, 128, device="cuda"))]):
+            for mode in ("selector", "sequential", "go"):
+                one.c.fill_(float("nan"))
+                ctx.execute([one.gemm] + [o.gemm for o in others] + add, mode=mode)
+                torch.cuda.synchronize()
+                assert torch.equal(one.c, ref[0]) and torch.equal(one.sums, ref[1])
+                for o in others:
+                    o.check()
+                for a in add:
+                    assert torch.equal(a.c, (a.a.float() + a.b.float()).to(a.c.dtype))
+
+
 @pytest.mark.parametrize("pad", [1, 3, 4, 8])
 def test_pitches(ctx, pad):
     for dtype in ("bf16", "f32", "fp8"):
