@@ -2,44 +2,60 @@
 // f'(z) and the column sums of dz (over all rows, or over the rows of each group),
 // and the sums that finish every bias gradient of the library.
 //
-// Bound by memory: dy and z are read once and dz written once, 16 bytes a lane, the
-// sums stay in registers over a workgroup's rows.  Sums over many rows are
-// split: each workgroup writes one row of partial sums, bias_sums or group_sums
-// adds them in order (no atomics: the result does not depend on the run).
+// Bound by memory: dy and z are read once and dz written once, 16 bytes a lane.  A
+// workgroup of 512 threads takes 32 rows, four a thread, all loaded before the first
+// is computed, and ends: workgroups that loop over 64 rows (256 threads) are all
+// resident at once and load, compute and store in step ((8192, 4096) bf16 gelu 54 us, 41.8
+// this way, 4.8 TB/s; 16 rows 40.7; with the column sums 55.6, 48.2 and 48.0; (16384, 8192)
+// silu 154, 138 and 136, with sums 161, 151 and 156: 16 rows write twice the partial sums).
+// Sums over many rows are split: each workgroup writes one row of partial sums,
+// bias_sums or group_sums adds them in order (no atomics: the result does not
+// depend on the run).
 #pragma once
 #include "grouped.h"
 
 namespace gdy {
 
-// 256 threads: 64 columns x 4 lanes of rows, added in order.
+// Sums of COLS columns by LANES lanes of rows, added in order.  Many rows: 16 x 64, so
+// that there are workgroups and rows in flight enough that each waits for memory
+// about once (512 rows of 4096: with its launch 6.8 us, as on 64 x 16); few rows: 64 x 4
+// (16 groups of about 6 rows of 1536: with the sums' kernel 16.4 us, on 16 x 64 22.6).
+template <int COLS, int LANES>
 __device__ __forceinline__ void column_sums(const float* part, float* out, int n, int rows, int col, float* lds) {
-  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
+  const int lane = threadIdx.x % COLS, q = threadIdx.x / COLS;
   const bool live = col + lane < n;
   float x = 0.0f;
   if (live) {
     const float* p = part + col + lane;
 #pragma unroll 8
-    for (int r = q; r < rows; r += 4) x += p[(int64_t)r * n];
+    for (int r = q; r < rows; r += LANES) x += p[(int64_t)r * n];
   }
   lds[threadIdx.x] = x;
   __syncthreads();
-  if (q == 0 && live) out[col + lane] = (lds[lane] + lds[64 + lane]) + (lds[128 + lane] + lds[192 + lane]);
+  if (q == 0 && live) {
+#pragma unroll
+    for (int w = 1; w < LANES; ++w) x += lds[w * COLS + lane];
+    out[col + lane] = x;
+  }
 }
 
-static __global__ void __launch_bounds__(256) bias_sums(BiasSums s) {
-  __shared__ float lds[256];
+template <int COLS, int LANES>
+__global__ void __launch_bounds__(COLS * LANES) bias_sums(BiasSums s) {
+  __shared__ float lds[COLS * LANES];
   int u = 0;
   while (u + 1 < s.count && (int)blockIdx.x >= s.first[u + 1]) ++u;
-  const int blocks = (s.n[u] + 63) / 64, b = (int)blockIdx.x - s.first[u];
+  const int blocks = (s.n[u] + COLS - 1) / COLS, b = (int)blockIdx.x - s.first[u];
   const int item = b / blocks;
-  column_sums(s.part[u] + (int64_t)item * s.rows[u] * s.n[u], s.out[u] + item * s.stride[u], s.n[u], s.rows[u],
-              (b - item * blocks) * 64, lds);
+  column_sums<COLS, LANES>(s.part[u] + (int64_t)item * s.rows[u] * s.n[u], s.out[u] + item * s.stride[u], s.n[u],
+                           s.rows[u], (b - item * blocks) * COLS, lds);
 }
 
 // The sums of group e, or of all groups (GroupSums::shared).
-static __global__ void __launch_bounds__(256) group_sums(GroupSums s) {
-  __shared__ float lds[256];
-  const int blocks = (s.n + 63) / 64, e = (int)blockIdx.x / blocks, col = ((int)blockIdx.x - e * blocks) * 64;
+template <int COLS, int LANES>
+__global__ void __launch_bounds__(COLS * LANES) group_sums(GroupSums s) {
+  __shared__ float lds[COLS * LANES];
+  const int blocks = (s.n + COLS - 1) / COLS, e = (int)blockIdx.x / blocks;
+  const int col = ((int)blockIdx.x - e * blocks) * COLS;
   int first = 0, count;
   if (s.shared) {
     count = total_slots(s.offsets, s.groups, s.rows, s.bm, s.max_slots);
@@ -48,14 +64,14 @@ static __global__ void __launch_bounds__(256) group_sums(GroupSums s) {
     const GroupRows g = group_rows(s.offsets, s.groups, s.rows, e);
     count = min((g.count + s.bm - 1) / s.bm, max(s.max_slots - first, 0));
   }
-  column_sums(s.part + (int64_t)first * s.per * s.n, s.out + e * s.stride, s.n, count * s.per, col, lds);
+  column_sums<COLS, LANES>(s.part + (int64_t)first * s.per * s.n, s.out + e * s.stride, s.n, count * s.per, col, lds);
 }
 
 // A workgroup: bm rows of a group x kActCols columns, a lane eight consecutive ones.
 template <int DT>
-__global__ void __launch_bounds__(256) act_grad(KActGrad g) {
-  constexpr int OS = OutSize<DT>::v, LPR = kActCols / 8, RP = 256 / LPR, AHEAD = 4;
-  __shared__ __attribute__((aligned(16))) float lds[256 * 8];
+__global__ void __launch_bounds__(kActThreads) act_grad(KActGrad g) {
+  constexpr int OS = OutSize<DT>::v, LPR = kActCols / 8, RP = kActThreads / LPR, AHEAD = kActRows / RP;
+  __shared__ __attribute__((aligned(16))) float lds[kActThreads * 8];
   const int tn = (g.n + kActCols - 1) / kActCols;
   const int slot = (int)blockIdx.x / tn, n0 = ((int)blockIdx.x - slot * tn) * kActCols;
   GroupSlot s = {0, 0, g.rows, 0};
@@ -106,7 +122,7 @@ __global__ void __launch_bounds__(256) act_grad(KActGrad g) {
 #pragma unroll
   for (int q = 0; q < 8; ++q) lds[(tid / LPR) * kActCols + c8 + q] = sum[q];
   __syncthreads();
-  for (int c = tid; c < cols; c += 256) {
+  for (int c = tid; c < cols; c += kActThreads) {
     float x = lds[c];
 #pragma unroll
     for (int r = 1; r < RP; ++r) x += lds[r * kActCols + c];

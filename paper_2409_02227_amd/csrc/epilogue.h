@@ -77,13 +77,11 @@ __device__ __forceinline__ float logistic2(float y) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y));
 }
 
-// exp(-x^2 / 2) and Phi(x), the normal distribution function.  With a = |x|,
-// Phi(-a) = exp(-a^2 / 2) Q(a), Q(a) = erfcx(a / sqrt 2) / 2, and Q as a polynomial
-// in t = 1 / (1 + 0.3 a), fitted to the least largest relative error on [0, 14]
-// (4.6e-7 evaluated in fp32): small Phi keep their relative precision, which 1 +
-// erf loses.
-__device__ __forceinline__ float normal_cdf(float x, float& bell) {
-  const float a = __builtin_fabsf(x);
+// exp(-a^2 / 2) and Q(a) = erfcx(a / sqrt 2) / 2 for a >= 0: the normal distribution
+// function is Phi(-a) = exp(-a^2 / 2) Q(a).  Q is a polynomial in t = 1 / (1 + 0.3 a),
+// fitted to the least largest relative error on [0, 14] (4.6e-7 evaluated in fp32):
+// small Phi keep their relative precision, which 1 + erf loses.
+__device__ __forceinline__ float mills(float a, float& bell) {
   const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, a, 1.0f));
   float q = 0.03567638332048663f;
   q = __builtin_fmaf(q, t, -0.15720967723673793f);
@@ -94,8 +92,7 @@ __device__ __forceinline__ float normal_cdf(float x, float& bell) {
   q = __builtin_fmaf(q, t, 0.12075420880971754f);
   q = __builtin_fmaf(q, t, 0.11962928249451463f);
   bell = __builtin_amdgcn_exp2f(a * a * (-0.5f * kLog2e));
-  q = q * t * bell;
-  return x < 0.0f ? q : 1.0f - q;
+  return q * t;
 }
 
 // (1 + tanh u) / 2 = logistic(2u), 2u = x (A + B x^2)
@@ -106,7 +103,8 @@ template <int ACT> __device__ __forceinline__ float act_value(float x) {
   if constexpr (ACT == ACT_RELU) return x < 0.0f ? 0.0f : x;  // NaN stays NaN
   if constexpr (ACT == ACT_GELU) {
     float bell;
-    return x * normal_cdf(x, bell);
+    const float q = mills(__builtin_fabsf(x), bell) * bell;
+    return x * (x < 0.0f ? q : 1.0f - q);
   }
   if constexpr (ACT == ACT_GELU_TANH) return x * logistic2(x * __builtin_fmaf(-kLog2e * kTanhB, x * x, -kLog2e * kTanhA));
   if constexpr (ACT == ACT_SILU) return x * logistic2(-kLog2e * x);
@@ -114,15 +112,20 @@ template <int ACT> __device__ __forceinline__ float act_value(float x) {
 }
 
 // f'(x).  Beyond +-64 every slope is 0 or 1 in fp32; the saved value may be
-// infinite where it passed its type's range, and inf * 0 must not enter.
+// infinite where it passed its type's range, and inf * 0 must not enter (NaN does).
 template <int ACT> __device__ __forceinline__ float act_slope(float x) {
-  x = x > 64.0f ? 64.0f : x < -64.0f ? -64.0f : x;
   if constexpr (ACT == ACT_RELU) return x <= 0.0f ? 0.0f : 1.0f;
   if constexpr (ACT == ACT_GELU) {
+    // Phi(x) + x phi(x) is w = phi's factor exp(-a^2 / 2) times (Q(a) - a / sqrt(2 pi))
+    // for x < 0, a = |x|, and 1 - w above
+    float a = __builtin_fabsf(x);
+    a = a > 64.0f ? 64.0f : a;
     float bell;
-    const float cdf = normal_cdf(x, bell);
-    return __builtin_fmaf(x * bell, 0.3989422804014327f, cdf);
+    const float q = mills(a, bell);
+    const float w = bell * __builtin_fmaf(a, -0.3989422804014327f, q);
+    return x < 0.0f ? w : 1.0f - w;
   }
+  x = x > 64.0f ? 64.0f : x < -64.0f ? -64.0f : x;
   if constexpr (ACT == ACT_GELU_TANH) {
     const float x2 = x * x, p = logistic2(x * __builtin_fmaf(-kLog2e * kTanhB, x2, -kLog2e * kTanhA));
     return __builtin_fmaf(x * p * (1.0f - p), __builtin_fmaf(3.0f * kTanhB, x2, kTanhA), p);

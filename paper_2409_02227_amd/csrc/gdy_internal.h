@@ -158,10 +158,17 @@ struct GroupKernel {
   int bm, bn, threads;
 };
 
+// The kernels that finish bias gradients: a workgroup's columns and threads, for sums of
+// many rows and of fewer than kSumManyRows.
+constexpr int kSumManyRows = 64;
+constexpr int sum_cols(bool many) { return many ? 16 : 64; }
+constexpr int sum_threads(bool many) { return many ? 1024 : 256; }
+
 // Partial sums to a bias gradient: out[item][j] = sum over `rows` rows of part.
 struct BiasSums {
   int32_t count;
-  int32_t first[kMaxFused + 1];  // workgroup ranges: 64 columns of an item each
+  int32_t many;                  // 1: some member has many rows
+  int32_t first[kMaxFused + 1];  // workgroup ranges: sum_cols() columns of an item each
   const float* part[kMaxFused];
   float* out[kMaxFused];
   int64_t stride[kMaxFused];     // between items of out
@@ -189,7 +196,7 @@ struct KActGrad {
   int32_t dy_vec, z_vec, dz_vec;
 };
 
-constexpr int kActCols = 512;  // columns of a workgroup
+constexpr int kActCols = 512, kActRows = 32, kActThreads = 512;  // of a workgroup
 
 // Compile-time description of one instantiated kernel.
 struct KernelDesc {
@@ -247,8 +254,8 @@ GroupKernel group_f16(int over_k, int tb, int tile);
 GroupKernel group_fp8(int over_k, int tb, int tile);
 GroupKernel group_f32(int over_k, int tb, int tile);
 const void* act_grad_kernel(int dt);  // null: no such type
-const void* bias_sum_kernel();
-const void* group_sum_kernel();
+const void* bias_sum_kernel(bool many);
+const void* group_sum_kernel(bool many);
 int kernels_d_bf16(const KernelDesc** out);
 int kernels_d_f16(const KernelDesc** out);
 int kernels_d_fp8(const KernelDesc** out);

@@ -8,5 +8,9 @@ const void* gdy::act_grad_kernel(int dt) {
     default: return nullptr;
   }
 }
-const void* gdy::bias_sum_kernel() { return reinterpret_cast<const void*>(&bias_sums); }
-const void* gdy::group_sum_kernel() { return reinterpret_cast<const void*>(&group_sums); }
+const void* gdy::bias_sum_kernel(bool many) {
+  return many ? reinterpret_cast<const void*>(&bias_sums<16, 64>) : reinterpret_cast<const void*>(&bias_sums<64, 4>);
+}
+const void* gdy::group_sum_kernel(bool many) {
+  return many ? reinterpret_cast<const void*>(&group_sums<16, 64>) : reinterpret_cast<const void*>(&group_sums<64, 4>);
+}

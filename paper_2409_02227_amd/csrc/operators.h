@@ -123,19 +123,37 @@ gdy_status validate_epilogues(gdy_ctx* ctx, const gdy_gemm* g, const gdy_epilogu
 // ---------------------------------------------------------------------------
 void add_bias_sum(BiasSums* s, const float* part, float* out, int n, int rows, int items, int64_t stride) {
   const int u = s->count++;
-  if (u == 0) s->first[0] = 0;
+  if (u == 0) s->many = 0;
   s->part[u] = part;
   s->out[u] = out;
   s->stride[u] = stride;
   s->n[u] = n;
   s->rows[u] = rows;
-  s->first[u + 1] = s->first[u] + items * ((n + 63) / 64);
+  s->first[u] = items;  // ranges are made at the launch
+  if (rows >= kSumManyRows) s->many = 1;
 }
 
 hipError_t launch_bias_sums(BiasSums* s, hipStream_t hs, hipEvent_t stop) {
   if (s->count == 0) return hipSuccess;
+  const int cols = sum_cols(s->many != 0);
+  int wg = 0;
+  for (int u = 0; u < s->count; ++u) {
+    const int items = s->first[u];
+    s->first[u] = wg;
+    wg += items * ((s->n[u] + cols - 1) / cols);
+  }
+  s->first[s->count] = wg;
   void* argv[] = {s};
-  return hipExtLaunchKernel(bias_sum_kernel(), dim3(s->first[s->count]), dim3(256), argv, 0, hs, nullptr, stop, 0);
+  return hipExtLaunchKernel(bias_sum_kernel(s->many != 0), dim3(wg), dim3(sum_threads(s->many != 0)), argv, 0, hs,
+                            nullptr, stop, 0);
+}
+
+hipError_t launch_group_sums(const GroupSums& s, hipStream_t hs) {
+  const bool many = (int64_t)s.max_slots * s.per / (s.shared ? 1 : std::max(s.groups, 1)) >= kSumManyRows;
+  const int64_t blocks = (s.n + sum_cols(many) - 1) / sum_cols(many);
+  void* argv[] = {(void*)&s};
+  return hipExtLaunchKernel(group_sum_kernel(many), dim3((unsigned)(blocks * (s.shared ? 1 : s.groups))),
+                            dim3(sum_threads(many)), argv, 0, hs, nullptr, nullptr, 0);
 }
 
 // Zeros to the bias gradients of members without rows, which no launch computes.
@@ -369,10 +387,7 @@ gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue
   if (bias_grad) {
     GroupSums s = {ctx->split_ws, bias_grad, g.offsets, ep->stride_bias_grad, a.n, a.rows, a.groups, a.bm,
                    a.max_slots, shared ? 1 : 0, sums_per_tile};
-    void* sargv[] = {&s};
-    const int64_t blocks = (g.n + 63) / 64;
-    HIP_TRY(ctx, hipExtLaunchKernel(group_sum_kernel(), dim3((unsigned)(blocks * (shared ? 1 : g.groups))), dim3(256),
-                                    sargv, 0, hs, nullptr, nullptr, 0));
+    HIP_TRY(ctx, launch_group_sums(s, hs));
   }
   return GDY_OK;
 }
@@ -456,19 +471,20 @@ gdy_status launch_act_grad(gdy_ctx* ctx, const gdy_act_grad& g, hipStream_t hs) 
   a.dz_vec = vec(g.dz, g.lddz);
   const int64_t tn = (g.n + kActCols - 1) / kActCols;
   auto slots = [&](int bm) { return g.offsets ? max_row_tiles(g.rows, groups, bm) : (g.rows + bm - 1) / bm; };
-  a.bm = slots(64) * tn >= 2 * ctx->cus ? 64 : 16;
+  a.bm = kActRows;
   a.max_slots = (int32_t)slots(a.bm);
   if (g.bias_grad) {
     const int64_t need = (int64_t)a.max_slots * g.n * 4;
     if (need > kSplitWsBytes)
       return fail(ctx, GDY_ERR_UNSUPPORTED, "act_grad: bias_grad needs %lld bytes of workspace, %lld are there",
                   (long long)need, (long long)kSplitWsBytes);
-    a.part = ctx->split_ws;
+    // one row tile: its sums are the bias gradient
+    a.part = !g.offsets && a.max_slots == 1 ? g.bias_grad : ctx->split_ws;
   }
   void* argv[] = {&a};
-  HIP_TRY(ctx, hipExtLaunchKernel(act_grad_kernel(g.type), dim3((unsigned)(a.max_slots * tn)), dim3(256), argv, 0, hs,
+  HIP_TRY(ctx, hipExtLaunchKernel(act_grad_kernel(g.type), dim3((unsigned)(a.max_slots * tn)), dim3(kActThreads), argv, 0, hs,
                                   nullptr, nullptr, 0));
-  if (!g.bias_grad) return GDY_OK;
+  if (!g.bias_grad || a.part == g.bias_grad) return GDY_OK;
   if (!g.offsets) {
     BiasSums s;
     s.count = 0;
@@ -477,9 +493,7 @@ gdy_status launch_act_grad(gdy_ctx* ctx, const gdy_act_grad& g, hipStream_t hs) 
   } else {
     GroupSums s = {a.part, g.bias_grad, g.offsets, g.stride_bias_grad, a.n, a.rows, groups, a.bm, a.max_slots,
                    shared ? 1 : 0, 1};
-    void* sargv[] = {&s};
-    HIP_TRY(ctx, hipExtLaunchKernel(group_sum_kernel(), dim3((unsigned)((g.n + 63) / 64 * (shared ? 1 : groups))), dim3(256),
-                                    sargv, 0, hs, nullptr, nullptr, 0));
+    HIP_TRY(ctx, launch_group_sums(s, hs));
   }
   return GDY_OK;
 }
