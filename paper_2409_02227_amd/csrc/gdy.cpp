@@ -1352,33 +1352,42 @@ bool use_rows128(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int
   return rows128_wins(launch_cus(ctx, p, mode, p.stream_of[members[0]]), g, members);
 }
 
-// The tile of a launch with epilogues whose members all run 128 x 128 tiles, uncapped,
-// and leave CUs without one: 64 x 128 (twice the workgroups, two a CU; unsplit
-// members), or for more than kDeepKTiles K tiles (kDeepRunTiles a run), where both
-// operands take copies, a ring of four stages of the same tile (0: as it is).  bf16 with weights from HBM, 128 x 128 tiles
-// of four stages against 64 x 128 ones of three: (1024, 4096, 1024) nt 19.6 and 17.1 us,
-// (512, 6144, 4096) nn 44.8 and 43.6, (512, 6144, 6144) 65 and 86, (512, 6144, 12288) 124 and
-// 161.  Neither changes an element's sum.
+// The tile of a launch with epilogues whose uncapped members all run 128 x 128 or all 64 x
+// 64 tiles and leave CUs without one (a joint tile index, or 5: the ring of four
+// stages; 0: as it is; bf16, weights from HBM, with a bias and silu):
+// * 128 x 128: 64 x 128 (twice the workgroups, two a CU; unsplit members of an
+//   untransposed A), or for more than kDeepKTiles K tiles (kDeepRunTiles a run), where both
+//   operands take copies, four stages of the same tile in place of two.  Four stages
+//   against 64 x 128: (1024, 4096, 1024) nt 19.6 and 17.1 us, (512, 6144, 4096) nn 44.8 and
+//   43.6, (512, 6144, 6144) 65 and 86, (512, 6144, 12288) 124 and 161.
+// * 64 x 64, unsplit: 32 x 64.  (64, 4096, 1024) nn 9.8 and 8.6, fp8 (512, 1024, 1000) nt 10.8
+//   and 8.9, fp16 (509, 2047, 1021) nn 17.6 and 17.5, gelu's slope 20.2 and 19.3.
+// None changes an element's sum.
 const int kDeepKTiles = 64, kDeepRunTiles = 32;
 int few_tiles(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int mode, const Members& members,
               int joint) {
-  int64_t tiles = 0;
-  bool deep = true, first = true, low = true;
-  int code = 0;
+  if (joint != 1) return 0;
+  int64_t items = 0;
+  bool deep = true, low = true, unsplit = true;
+  int code = -1;
   for (int i : members) {
     if (is_add_variant(ctx, p.variant_of[i])) continue;
     const Exec e = joint_exec(ctx, p.variant_of[i], g[i], joint);
-    if (joint != 1 || e.family != 1 || (e.code & 7) != 0 || ctx->variants[p.variant_of[i]].cap > 0) return 0;
+    const int tile = e.code & 7;
+    if (e.family != 1 || (tile != 0 && tile != 2) || (code >= 0 && tile != (code & 7)) ||
+        ctx->variants[p.variant_of[i]].cap > 0)
+      return 0;
     const int split = std::max(p.split_of[i], 1);
-    deep = deep && a_copies(g[i]) && b_copies(g[i]) && (first || e.code == code) &&
+    deep = deep && a_copies(g[i]) && b_copies(g[i]) && (code < 0 || e.code == code) &&
            g[i].k * elem_size(g[i].a_type) / split > (split > 1 ? kDeepRunTiles : kDeepKTiles) * kTileKBytes;
-    low = low && !g[i].trans_a && split == 1;
-    first = false;
+    low = low && !g[i].trans_a;
+    unsplit = unsplit && split == 1;
     code = e.code;
-    tiles += (g[i].m + 127) / 128 * ((g[i].n + 127) / 128) * std::max(g[i].batch, 1) * split;
+    items += (g[i].m + e.jbm - 1) / e.jbm * ((g[i].n + e.jbn - 1) / e.jbn) * std::max(g[i].batch, 1) * split;
   }
-  if (tiles > launch_cus(ctx, p, mode, p.stream_of[members[0]])) return 0;
-  return deep ? 5 : low ? 1 : 0;
+  if (code < 0 || items > launch_cus(ctx, p, mode, p.stream_of[members[0]])) return 0;
+  if ((code & 7) == 2) return unsplit ? 4 : 0;
+  return deep ? 5 : low && unsplit ? 1 : 0;
 }
 
 // Workgroup ranges of one dispatch: each GEMM gets its own grid (tiles, or
@@ -1403,8 +1412,8 @@ gdy_status build_launch(gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, in
     const KernelDesc* d = ctx->kernels[v.kernel].d;
     Exec e = joint ? joint_exec(ctx, p.variant_of[i], g[i], joint) : exec_of(ctx, p.variant_of[i], g[i]);
     if (few && !d->ew) {
-      e.code += few;
-      if (few == 1) e.jbm = 64;
+      e.code = (e.code & ~7) + few;
+      e.jbm = few == 1 ? 64 : few == 4 ? 32 : 128;
     } else if (epilogues && joint == 1 && !d->ew && (e.code & 7) == 4) {
       e.jbm = 32;  // 16-row tiles: 32 rows and four stages there
     }
@@ -1599,11 +1608,12 @@ bool skinny(const gdy_gemm& g, const gdy_epilogue& e) {
 }
 
 // Rows of partial column sums that an item of g may take: its tile rows, or those
-// of the split reduction.  Members of larger tiles may run 128- or 64-row ones.
+// of the split reduction.  Members may run on tiles of fewer rows than their kernel's.
 int64_t part_rows(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
   if (p.split_of[i] > 1) return (g.m + kEpiReduceRows - 1) / kEpiReduceRows;
   int bm = std::min(exec_of(ctx, p.variant_of[i], g).jbm, 128);
   if (bm == 128) bm = 64;  // few_tiles
+  else if (bm == 64) bm = 32;
   return (g.m + bm - 1) / bm;
 }
 int64_t part_bytes(const gdy_ctx* ctx, const gdy_gemm& g, const gdy_plan_t& p, int i) {
