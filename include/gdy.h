@@ -317,7 +317,9 @@ gdy_status gdy_execute_static(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, in
  *                  layer below added to aux.
  * f: the identity, max(z, 0), z Phi(z) (the normal distribution function), z (1 +
  * tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2, or z / (1 + exp(-z)).  The slope of
- * GDY_ACT_RELU at 0 is 0.  A zeroed struct is no epilogue.
+ * GDY_ACT_RELU at 0 is 0.  f of minus infinity is what the formula gives in floating
+ * point (NaN but for GDY_ACT_RELU and GDY_ACT_NONE), slopes at infinities are the limits, 0
+ * and 1.  A zeroed struct is no epilogue.
  */
 typedef enum {
   GDY_ACT_NONE = 0,
@@ -335,7 +337,7 @@ typedef struct {
   int32_t reserved;                 /* must be 0                                            */
   const void* residual; int64_t ldr;    /* R: M x N of C's type, or NULL; ldr >= n          */
   void* aux;            int64_t ldaux;  /* M x N of C's type, or NULL; ldaux >= n           */
-  float* bias_grad;                 /* N values, or NULL; overwritten                       */
+  float* bias_grad;                 /* N values, or NULL; overwritten; at most 2^26 in all   */
   /* between items of a strided batch (or groups, gdy_execute_grouped), in elements: bias 0
    * shares one bias, bias_grad 0 adds the items' sums up.  Ignored for a single GEMM. */
   int64_t stride_bias, stride_r, stride_aux, stride_bias_grad;
@@ -346,10 +348,15 @@ typedef struct {
  * host array of n, read during the call only; NULL: no epilogues, exactly
  * gdy_execute).  The plan is gdy_execute's for the same GEMMs, and every mode takes
  * them; members with and without epilogues mix, and adds (GDY_OP_ADD) must have
- * none.  R may be C itself (same pointer, ldr = ldc, stride_r = stride_c), as may
- * a backward pass's aux; otherwise no output (C, a written aux, bias_grad) may
- * overlap anything else that the submission reads or writes.  k = 0 gives z =
- * bias; m = 0 writes nothing but a bias_grad of zeros.
+ * none.  k = 0 gives z = bias; m = 0 writes nothing but a bias_grad of zeros.
+ * A GEMM's fp32 sums are those of its plain launch, whatever runs beside it.  GEMMs
+ * with an epilogue of at most 16 rows, an untransposed A, 16-byte aligned operands
+ * and a short K (at most 8 KiB of a row of A, 4 KiB where B is not transposed) run
+ * on a kernel of their own whatever kernel and split the plan names, which adds in
+ * another order, alone and beside others alike.
+ * R may be C itself (same pointer, ldr = ldc, stride_r = stride_c), as may a backward
+ * pass's aux; otherwise no output (C, a written aux, bias_grad) may overlap anything
+ * else that the submission reads or writes.
  * Every pointer is aligned to its elements.  The split-K workspace also holds the
  * partial column sums of a group's bias gradients: a group that needs more of both
  * than the workspace has is refused (GDY_ERR_UNSUPPORTED) before anything launches.

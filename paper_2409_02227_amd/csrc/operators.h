@@ -19,8 +19,16 @@ struct Range {
 Extent matrix_range(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t items, int64_t stride, int es) {
   if (!p || rows <= 0 || cols <= 0 || items <= 0) return Extent{0, 0};
   const uintptr_t lo = (uintptr_t)p;
-  return Extent{lo, lo + (uintptr_t)(((items - 1) * stride + (rows - 1) * ld + cols) * es)};
+  const __int128 bytes = ((__int128)(items - 1) * stride + (__int128)(rows - 1) * ld + cols) * es;
+  return Extent{lo, bytes > (__int128)(UINTPTR_MAX - lo) ? UINTPTR_MAX : lo + (uintptr_t)bytes};
 }
+
+// Strides between items in elements, far inside what 64-bit byte offsets hold.
+const int64_t kMaxStride = (int64_t)1 << 44;
+
+// Values of a bias_grad: sums of 2^26 columns, of all members of a submission, are one
+// launch of fewer than 2^32 threads.
+const int64_t kMaxBiasGrad = (int64_t)1 << 26;
 
 gdy_status check_ranges(gdy_ctx* ctx, const std::vector<Range>& r) {
   for (size_t i = 0; i < r.size(); ++i) {
@@ -67,6 +75,12 @@ gdy_status validate_epilogue(gdy_ctx* ctx, const gdy_epilogue& e, const EpiTarge
     return fail(ctx, GDY_ERR_INVALID_ARG, "%s %d: negative epilogue stride", t.what, t.index);
   if (groups && e.bias_grad && e.stride_bias_grad != 0 && e.stride_bias_grad < t.n)
     return fail(ctx, GDY_ERR_ALIAS, "%s %d: items of bias_grad overlap", t.what, t.index);
+  if ((many && ((e.residual && e.stride_r > kMaxStride) || (e.aux && e.stride_aux > kMaxStride))) ||
+      (groups && ((e.bias && e.stride_bias > kMaxStride) || (e.bias_grad && e.stride_bias_grad > kMaxStride))))
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "%s %d: epilogue stride too large", t.what, t.index);
+  if (e.bias_grad && t.n > kMaxBiasGrad / (groups && e.stride_bias_grad ? t.biases : 1))
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "%s %d: bias_grad of more than %lld values", t.what, t.index,
+                (long long)kMaxBiasGrad);
   // 32-bit byte offsets up to 256 rows past the edge, within an item (grouped rows: a tile)
   const int64_t tile_rows = std::min<int64_t>(t.m, t.stride_c < 0 ? 256 : t.m);
   int64_t bytes;
@@ -206,6 +220,8 @@ gdy_status validate_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilog
     return fail(ctx, GDY_ERR_UNSUPPORTED, "grouped: sizes too large");
   if (!g.offsets || (uintptr_t)g.offsets % 4 || (uintptr_t)g.scales % 4)
     return fail(ctx, GDY_ERR_INVALID_ARG, "grouped: null or unaligned offsets or scales");
+  if (g.groups > 1 && (over_k ? g.stride_c : g.stride_b) > kMaxStride)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "grouped: stride too large");
   std::vector<Range> ranges;
   ranges.push_back({matrix_range(g.offsets, 1, g.groups + 1, 0, 1, 0, 4), false, 0});
   ranges.push_back({matrix_range(g.scales, 1, g.groups, 0, 1, 0, 4), false, 0});
@@ -382,6 +398,8 @@ gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue
   const int64_t tn = (g.n + kern.bn - 1) / kern.bn;
   const int64_t grid = over_k ? (((m + kern.bm - 1) / kern.bm * tn + kXcds - 1) / kXcds) * kXcds * g.groups
                               : (((int64_t)a.max_slots * tn + kXcds - 1) / kXcds + a.xcd_cus / 2) * kXcds;
+  if (grid * kern.threads > UINT32_MAX)  // threads of a launch
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "grouped: a grid of %lld workgroups", (long long)grid);
   void* argv[] = {&a};
   HIP_TRY(ctx, hipExtLaunchKernel(kern.func, dim3((unsigned)grid), dim3(kern.threads), argv, 0, hs, nullptr, nullptr, 0));
   if (bias_grad) {
@@ -413,6 +431,10 @@ gdy_status validate_act_grad(gdy_ctx* ctx, const gdy_act_grad& g) {
   const int64_t groups = g.offsets ? g.groups : 1;
   if (g.bias_grad && groups > 1 && g.stride_bias_grad != 0 && g.stride_bias_grad < g.n)
     return fail(ctx, g.stride_bias_grad < 0 ? GDY_ERR_INVALID_ARG : GDY_ERR_ALIAS, "act_grad: bad stride_bias_grad");
+  if (g.bias_grad && groups > 1 && g.stride_bias_grad > kMaxStride)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "act_grad: stride_bias_grad too large");
+  if (g.bias_grad && g.n > kMaxBiasGrad / (groups > 1 && g.stride_bias_grad ? groups : 1))
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "act_grad: bias_grad of more than %lld values", (long long)kMaxBiasGrad);
   if (g.rows > INT32_MAX - 4096 || g.n > INT32_MAX - 4096 ||
       ((g.rows + 15) / 16 + groups) * ((g.n + kActCols - 1) / kActCols) > INT32_MAX / 2)
     return fail(ctx, GDY_ERR_UNSUPPORTED, "act_grad: sizes too large");
@@ -481,6 +503,8 @@ gdy_status launch_act_grad(gdy_ctx* ctx, const gdy_act_grad& g, hipStream_t hs) 
     // one row tile: its sums are the bias gradient
     a.part = !g.offsets && a.max_slots == 1 ? g.bias_grad : ctx->split_ws;
   }
+  if ((int64_t)a.max_slots * tn * kActThreads > UINT32_MAX)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "act_grad: a grid of %lld workgroups", (long long)(a.max_slots * tn));
   void* argv[] = {&a};
   HIP_TRY(ctx, hipExtLaunchKernel(act_grad_kernel(g.type), dim3((unsigned)(a.max_slots * tn)), dim3(kActThreads), argv, 0, hs,
                                   nullptr, nullptr, 0));

@@ -172,6 +172,13 @@ def run_epilogue(ctx, gemms, epilogues, mode=gdy.SELECTOR, static=False):
     ({"batch": 3, "stride_c": 64 * 96}, {"stride_aux": 64 * 96, "stride_bias": -96}, INVALID),
     ({"batch": 3, "stride_c": 64 * 96}, {"stride_aux": 64 * 96, "stride_bias_grad": 95}, ALIAS),
     ({"batch": 3, "stride_c": 64 * 96}, {"stride_aux": 64 * 96, "stride_bias_grad": 96}, OK),
+    # strides and sums past what the launches' byte offsets and threads hold
+    ({"batch": 3, "stride_c": 64 * 96}, {"stride_aux": 64 * 96, "stride_r": 1 << 62}, UNSUPPORTED),
+    ({"batch": 3, "stride_c": 64 * 96}, {"stride_aux": (1 << 63) - 1}, UNSUPPORTED),
+    ({"batch": 3, "stride_c": 64 * 96}, {"stride_aux": 64 * 96, "stride_bias": 1 << 61}, UNSUPPORTED),
+    ({"batch": 3, "stride_c": 64 * 96}, {"stride_aux": 64 * 96, "stride_bias_grad": 1 << 61}, UNSUPPORTED),
+    ({"batch": 1 << 20, "stride_c": 64 * 96, "c": 1 << 42},
+     {"aux": None, "stride_bias_grad": 96, "residual": None, "bias_grad": 1 << 41}, UNSUPPORTED),
     # sizes of nothing
     ({"m": 0}, {"residual": None, "aux": None}, OK), ({"m": 0}, {"bias_grad": BASE + 2}, UNSUPPORTED),
     ({"n": 0}, {"bias_grad": 3}, OK), ({"k": 0}, {}, OK),
@@ -244,6 +251,9 @@ ONLY_R = {"act": 0, "bias": None, "aux": None, "bias_grad": None}
     ({"rows": 1 << 24, "a": 1 << 40, "c": 2 << 40}, None, OK), ({"rows": (1 << 31) - 4096}, None, UNSUPPORTED),
     ({"over": 1, "rows": 1 << 24}, None, UNSUPPORTED), ({"lda": 1 << 22}, None, UNSUPPORTED), ({"lda": 1 << 20, "a": 1 << 40}, None, OK),
     ({"ldc": 1 << 22}, None, UNSUPPORTED), ({"ldb": 1 << 23, "stride_b": 1 << 40, "b": 1 << 45}, None, UNSUPPORTED),
+    ({"stride_b": 1 << 62}, None, UNSUPPORTED), ({"over": 1, "stride_c": (1 << 63) - 1}, None, UNSUPPORTED),
+    ({"groups": 4096, "rows": 0, "n": 1 << 15, "k": 0, "c": None},
+     dict(ONLY_R, residual=None, stride_bias_grad=1 << 15, bias_grad=1 << 41), UNSUPPORTED),
     # epilogues
     ({}, {"act": 7}, INVALID), ({}, {"ldr": 95}, INVALID), ({}, {"stride_bias": -1}, INVALID),
     ({}, {"stride_bias_grad": 10}, ALIAS), ({}, {"stride_bias_grad": 96}, OK), ({}, {"grad": 1, "aux": None}, INVALID),
@@ -282,6 +292,9 @@ def act_grad(**kw):
     ({"bias_grad": BASE + (3 << 24) + 2}, UNSUPPORTED), ({"stride_bias_grad": 0}, OK), ({"stride_bias_grad": 95}, ALIAS),
     ({"stride_bias_grad": -96}, INVALID), ({"dz": BASE}, OK), ({"dz": BASE + (1 << 24)}, OK), ({"dz": BASE + 2}, ALIAS),
     ({"dz": BASE, "lddz": 100}, ALIAS), ({"bias_grad": BASE}, ALIAS), ({"dz": BASE + (30 << 24)}, ALIAS),
+    ({"stride_bias_grad": 1 << 62}, UNSUPPORTED),
+    ({"rows": 0, "groups": 4096, "n": 1 << 15, "stride_bias_grad": 1 << 15, "bias_grad": 1 << 41}, UNSUPPORTED),
+    ({"rows": 0, "groups": 4096, "n": 1 << 14, "stride_bias_grad": 1 << 14, "bias_grad": 1 << 41}, OK),
     ({"rows": 0, "dy": None}, OK), ({"n": 0}, OK), ({"rows": (1 << 31) - 4096}, UNSUPPORTED), ({"ldz": 1 << 23}, UNSUPPORTED),
 ])
 def test_act_grad_checks(ctx, g, want):
