@@ -32,6 +32,11 @@ struct EpiOut {
   float* part;  // the tile's row of column sums (null: none)
   int ldr, ldaux, act;
   bool bias_f32, grad, res_vec, aux_vec;
+  // C = round(scale * sum + bias) alone: the rounded tile goes through LDS as the plain
+  // kernels', two bytes an element and whole rows a store ((4813, 8064, 320) bf16 on
+  // 128 x 128 tiles: 56.6 us by EpiWave, 46.3 this way, 41.9 without a bias; over K, 64
+  // groups of 1024 rows in all, 2048 x 1024 each: 100 and 77).
+  __device__ __forceinline__ bool linear() const { return act == ACT_NONE && !res && !aux && !part; }
 };
 
 // Kernels without epilogues.
@@ -44,8 +49,10 @@ struct NoEpi {
 // there, which would otherwise load the fields before the tile loop and keep them
 // in registers through it (scalars then spill to scratch memory).
 // AHEAD: the rows whose residual and saved pre-activation a wave loads together.
-template <int AHEAD> struct MemberEpi {
-  static constexpr bool on = true;
+// LINEAR: whether linear epilogues have a path of their own (not in the kernels of mixed
+// 256 x 256 or fp8 members, whose registers it would pass).
+template <int AHEAD, bool LINEAR = true> struct MemberEpi {
+  static constexpr bool on = true, linear = LINEAR;
   static constexpr int ahead = AHEAD;
   static constexpr int kAt = (sizeof(KLaunch) + alignof(KEpis) - 1) / alignof(KEpis) * alignof(KEpis);
   typedef const __attribute__((address_space(4))) uint8_t* Ptr;
@@ -233,6 +240,31 @@ __device__ __forceinline__ void load_bias(const EpiOut& o, int j, float (&b)[8])
 #pragma unroll
     for (int q = 0; q < 8; ++q) b[q] = w.get(q);
   }
+}
+
+// The bias of columns j .. j + 3, and four of a linear epilogue's sums, rounded (two bytes
+// an element).
+template <int DT> __device__ __forceinline__ f32x4 load_bias4(const EpiOut& o, int j) {
+  constexpr int OS = OutSize<DT>::v;
+  f32x4 b = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (!o.bias) return b;
+  if (o.bias_f32) {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(o.bias, o.n * 4), j * 4, 0, 0));
+  } else {
+    const Rsrc r = make_rsrc(o.bias, o.n * OS);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) b[q] = ew_decode<Row8<DT>::OT>(load_elem<OS>(r, (j + q) * OS));
+    return b;
+  }
+}
+template <int DT> __device__ __forceinline__ f32x4 linear_sums(f32x4 x, float scale, f32x4 b) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) x[q] = DT == DT_FP8 ? __builtin_fmaf(x[q], scale, b[q]) : x[q] + b[q];
+  return x;
+}
+template <int DT> __device__ __forceinline__ u32x2 linear4(f32x4 x, float scale, f32x4 b) {
+  x = linear_sums<DT>(x, scale, b);
+  return u32x2{to_out2<Row8<DT>::OT>(x[0], x[1]), to_out2<Row8<DT>::OT>(x[2], x[3])};
 }
 
 // What a wave does with blocks of R rows x WC columns of a tile's sums, one after

@@ -283,40 +283,63 @@ __device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds
     if constexpr (EP::on) {  // a wave's quadrants one after another, by columns
       typedef EpiWave<DT, 64, 32, EP::ahead> Epi;
       static_assert(8 * Epi::BYTES + 2 * Epi::RP * 256 * 4 <= kPLds, "blocks and sums fit in the ring");
-      Epi x(ep(item, tm), lane);
-      lds_u8* block = smem + wave * Epi::BYTES;
-      auto dump = [&](const Acc (&h)[2][4]) {
+      const EpiOut o = ep(item, tm);
+      if (EP::linear && o.linear()) {  // as the plain launch, with a bias
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            *(__attribute__((address_space(3))) f32x4*)(block + (i * 16 + (lane & 15)) * Epi::PITCH +
-                                                        (j * 16 + 4 * (lane >> 4)) * 4) = h[j][i];
-      };
-      lds_u8* table = smem + 8 * Epi::BYTES;
-      auto put_sums = [&](int hb) {
-        x.put_sums(table, wm * Epi::RP + lane / Epi::LPR, 256, hb * 128 + wn * 32 + (lane % Epi::LPR) * 8);
-      };
-#pragma unroll 1
-      for (int q = 0; q < 4; ++q) {
-        const int ha = q & 1, hb = q >> 1;
-        if (ha == 0) {
-          if (hb && x.o.part) put_sums(0);
-          x.columns(n0 + hb * 128 + wn * 32);
-        } else if (half) {
-          continue;
-        }
-        if (q == 0) dump(acc[0][0]);
-        else if (q == 1) dump(acc[1][0]);
-        else if (q == 2) dump(acc[0][1]);
-        else dump(acc[1][1]);
-        const int m = m0 + ha * 128 + wm * 64;
-        x.rows(block, m, Mrows - m);
-      }
-      if (x.o.part) {
-        put_sums(1);
+          for (int j = 0; j < 2; ++j) {
+            const int col = hb * 128 + wn * 32 + j * 16 + 4 * (lane >> 4);
+            const f32x4 b = load_bias4<DT>(o, n0 + col);
+#pragma unroll
+            for (int ha = 0; ha < 2; ++ha) {
+              if (ha && half) break;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                *(__attribute__((address_space(3))) u32x2*)(smem + (ha * 128 + wm * 64 + i * 16 + (lane & 15)) * kPOutRow +
+                                                            col * 2) = linear4<DT>(acc[ha][hb][j][i], o.scale, b);
+            }
+          }
         __syncthreads();
-        add_sums<2 * Epi::RP>(table, 256, x.o.part + n0, min(256, Ncols - n0), (int)threadIdx.x);
+        store_tile<256, 512, kPOutRow>(smem, make_rsrc(o.c, o.c_bytes), (m0 * o.ldc + n0) * 2, o.ldc * 2,
+                                       min(half ? 128 : 256, Mrows - m0), min(256, Ncols - n0), o.c_vec,
+                                       (int)threadIdx.x);
+      } else {
+        Epi x(o, lane);
+        lds_u8* block = smem + wave * Epi::BYTES;
+        auto dump = [&](const Acc (&h)[2][4]) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              *(__attribute__((address_space(3))) f32x4*)(block + (i * 16 + (lane & 15)) * Epi::PITCH +
+                                                          (j * 16 + 4 * (lane >> 4)) * 4) = h[j][i];
+        };
+        lds_u8* table = smem + 8 * Epi::BYTES;
+        auto put_sums = [&](int hb) {
+          x.put_sums(table, wm * Epi::RP + lane / Epi::LPR, 256, hb * 128 + wn * 32 + (lane % Epi::LPR) * 8);
+        };
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+          const int ha = q & 1, hb = q >> 1;
+          if (ha == 0) {
+            if (hb && x.o.part) put_sums(0);
+            x.columns(n0 + hb * 128 + wn * 32);
+          } else if (half) {
+            continue;
+          }
+          if (q == 0) dump(acc[0][0]);
+          else if (q == 1) dump(acc[1][0]);
+          else if (q == 2) dump(acc[0][1]);
+          else dump(acc[1][1]);
+          const int m = m0 + ha * 128 + wm * 64;
+          x.rows(block, m, Mrows - m);
+        }
+        if (x.o.part) {
+          put_sums(1);
+          __syncthreads();
+          add_sums<2 * Epi::RP>(table, 256, x.o.part + n0, min(256, Ncols - n0), (int)threadIdx.x);
+        }
       }
     } else {
     const float s = p.scale;

@@ -462,27 +462,61 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
       constexpr int R = WTM < 32 ? WTM : 32;
       typedef EpiWave<DT, R, WTN, EP::ahead> Epi;
       static_assert(C::NW * Epi::BYTES <= C::LDS && WM * Epi::RP * BN * 4 <= C::LDS, "blocks and sums fit in the ring");
-      Epi x(ep(item, tm), lane);
-      lds_u8* block = smem + wave * Epi::BYTES;
-      x.columns(n0 + wn * WTN);
-#pragma unroll 1
-      for (int h = 0; h < WTM / R; ++h) {
+      const EpiOut o = ep(item, tm);
+      if (EP::linear && o.linear()) {  // as the plain launch, with a bias
+        const Rsrc rco = make_rsrc(o.c, o.c_bytes);
 #pragma unroll
-        for (int i = 0; i < C::FM; ++i) {
-          if (i / (R / 16) != h) continue;
+        for (int j = 0; j < C::FN; ++j) {
+          const int col = wn * WTN + j * 16 + 4 * (lane >> 4);
+          const f32x4 b = load_bias4<DT>(o, n0 + col);
 #pragma unroll
-          for (int j = 0; j < C::FN; ++j)
-            *(__attribute__((address_space(3))) f32x4*)(block + ((i % (R / 16)) * 16 + (lane & 15)) * Epi::PITCH +
-                                                        (j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i];
+          for (int i = 0; i < C::FM; ++i) {
+            const int row = wm * WTM + i * 16 + (lane & 15);
+            if constexpr (C::ES == 4) {
+              if (m0 + row >= Mrows) continue;
+              const f32x4 x = linear_sums<DT>(acc[j][i], o.scale, b);
+              const int off = ((m0 + row) * o.ldc + n0 + col) * 4;
+              if (n0 + col + 4 <= Ncols) {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), rco, off, 0, 0);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (n0 + col + e < Ncols) store_out<DT>(x[e], rco, off + 4 * e);
+              }
+            } else {
+              *(__attribute__((address_space(3))) u32x2*)(smem + row * C::PITCH + col * 2) =
+                  linear4<DT>(acc[j][i], o.scale, b);
+            }
+          }
         }
-        const int m = m0 + wm * WTM + h * R;
-        x.rows(block, m, Mrows - m);
-      }
-      if (x.o.part) {
-        __syncthreads();
-        x.put_sums(smem, wm * Epi::RP + lane / Epi::LPR, BN, wn * WTN + (lane % Epi::LPR) * 8);
-        __syncthreads();
-        add_sums<WM * Epi::RP>(smem, BN, x.o.part + n0, min(BN, Ncols - n0), tid);
+        if constexpr (C::ES != 4) {
+          __syncthreads();
+          store_tile<BN, C::NW * 64, C::PITCH>(smem, rco, (m0 * o.ldc + n0) * 2, o.ldc * 2, min(BM, Mrows - m0),
+                                               min(BN, Ncols - n0), o.c_vec, tid);
+        }
+      } else {
+        Epi x(o, lane);
+        lds_u8* block = smem + wave * Epi::BYTES;
+        x.columns(n0 + wn * WTN);
+#pragma unroll 1
+        for (int h = 0; h < WTM / R; ++h) {
+#pragma unroll
+          for (int i = 0; i < C::FM; ++i) {
+            if (i / (R / 16) != h) continue;
+#pragma unroll
+            for (int j = 0; j < C::FN; ++j)
+              *(__attribute__((address_space(3))) f32x4*)(block + ((i % (R / 16)) * 16 + (lane & 15)) * Epi::PITCH +
+                                                          (j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i];
+          }
+          const int m = m0 + wm * WTM + h * R;
+          x.rows(block, m, Mrows - m);
+        }
+        if (x.o.part) {
+          __syncthreads();
+          x.put_sums(smem, wm * Epi::RP + lane / Epi::LPR, BN, wn * WTN + (lane % Epi::LPR) * 8);
+          __syncthreads();
+          add_sums<WM * Epi::RP>(smem, BN, x.o.part + n0, min(BN, Ncols - n0), tid);
+        }
       }
     } else {
     const float s = p.scale;

@@ -100,7 +100,7 @@ __device__ __forceinline__ void group_tile(int t, int tm, int tn, int& i, int& j
 // A tile of a grouped product, and where its results go.  As MemberEpi, the argument
 // block is read again when the sums are done.
 struct GroupEpi {
-  static constexpr bool on = true;
+  static constexpr bool on = true, linear = true;
   static constexpr int ahead = 2;
   int e, row, n0, m, n, slot;  // group, first row and column in C, extent, row of partial sums
   int os;                      // bytes of an element of C
