@@ -85,7 +85,8 @@ __global__ void __launch_bounds__(kActThreads) act_grad(KActGrad g) {
   };
   const Rsrc ry = tile(g.dy, g.lddy), rz = tile(g.z, g.ldz), rd = tile(g.dz, g.lddz);
   const int tid = threadIdx.x, c8 = (tid % LPR) * 8, left = cols - c8;
-  const bool y_vec = OS == 4 || g.dy_vec, z_vec = OS == 4 || g.z_vec, d_vec = OS == 4 || g.dz_vec;
+  const bool whole = left >= 8, y_vec = whole && (OS == 4 || g.dy_vec), z_vec = whole && (OS == 4 || g.z_vec),
+             d_vec = whole && (OS == 4 || g.dz_vec);
   float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
   if (left > 0) {
     for (int r0 = tid / LPR; r0 < m; r0 += RP * AHEAD) {

@@ -174,9 +174,10 @@ template <int DT> struct Row8 {
   static constexpr int OS = OutSize<DT>::v, W = OS / 2;
   static constexpr int OT = DT == DT_FP8 ? DT_BF16 : DT;  // type of C
   u32x4 w[W];
-  // byte offset `off`; the first `left` columns lie inside the matrix
+  // byte offset `off`; the first `left` columns lie inside the matrix (vec: all eight, or
+  // `off` is out of range)
   __device__ __forceinline__ void load(Rsrc r, int off, bool vec, int left) {
-    if (vec && left >= 8) {
+    if (vec) {
 #pragma unroll
       for (int q = 0; q < W; ++q) w[q] = __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * q, 0, 0);
     } else {
@@ -205,7 +206,7 @@ template <int DT> struct Row8 {
     }
   }
   __device__ __forceinline__ void store(Rsrc r, int off, bool vec, int left) const {
-    if (vec && left >= 8) {
+    if (vec) {
 #pragma unroll
       for (int q = 0; q < W; ++q) __builtin_amdgcn_raw_buffer_store_b128(w[q], r, off + 16 * q, 0, 0);
     } else {
@@ -284,6 +285,7 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
   int lane;
   int col, left;  // this lane's first column, and how many of its eight lie inside C
   bool grad;
+  bool whole;     // every lane of the wave has all its columns inside C, or none
   float b[8], sum[8];
 
   __device__ __forceinline__ EpiWave(const EpiOut& out, int lane_) : o(out), lane(lane_) {
@@ -296,18 +298,22 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
   __device__ __forceinline__ void columns(int first) {
     col = first + (lane % LPR) * 8;
     left = o.n - col;
+    whole = __ballot(left > 0 && left < 8) == 0;
     load_bias<DT>(o, col, b);
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum[q] = 0.0f;
   }
 
-  __device__ __forceinline__ void load_inputs(int row, Row8<DT>& res, Row8<DT>& aux) {
-    if (o.res) res.load(rr, (row * o.ldr + col) * OS, OS == 4 || o.res_vec, left);
-    if (grad) aux.load(ra, (row * o.ldaux + col) * OS, OS == 4 || o.aux_vec, left);
+  // Byte offset of this lane's columns in a row; out of every range where `in` is false.
+  __device__ __forceinline__ int at(bool in, int row, int ld) const { return in ? (row * ld + col) * OS : kOutOfRange; }
+
+  __device__ __forceinline__ void load_inputs(bool in, int row, Row8<DT>& res, Row8<DT>& aux) {
+    if (o.res) res.load(rr, at(in, row, o.ldr), whole && (OS == 4 || o.res_vec), left);
+    if (grad) aux.load(ra, at(in, row, o.ldaux), whole && (OS == 4 || o.aux_vec), left);
   }
 
   // Eight sums of a row to C.
-  __device__ __forceinline__ void finish(int row, float (&x)[8], const Row8<DT>& res, const Row8<DT>& aux) {
+  __device__ __forceinline__ void finish(bool in, int row, float (&x)[8], const Row8<DT>& res, const Row8<DT>& aux) {
     Row8<DT> w;
 #pragma unroll
     for (int q = 0; q < 8; ++q) x[q] = DT == DT_FP8 ? __builtin_fmaf(x[q], o.scale, b[q]) : x[q] + b[q];
@@ -318,7 +324,7 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
     } else if (!o.grad) {
       if (o.aux) {
         w.set(x);
-        w.store(ra, (row * o.ldaux + col) * OS, OS == 4 || o.aux_vec, left);
+        w.store(ra, at(in, row, o.ldaux), whole && (OS == 4 || o.aux_vec), left);
       }
       apply_values(x, o.act);
     }
@@ -328,15 +334,17 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
     }
     if (o.part) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q) sum[q] += x[q];
+      for (int q = 0; q < 8; ++q) sum[q] += in ? x[q] : 0.0f;
     }
     w.set(x);
-    w.store(rc, (row * o.ldc + col) * OS, OS == 4 || o.c_vec, left);
+    w.store(rc, at(in, row, o.ldc), whole && (OS == 4 || o.c_vec), left);
   }
 
-  // The block at `block`: rows m0, m0 + 1, ... of C, which has `inside` from m0 on.
+  // The block at `block`: rows m0, m0 + 1, ... of C, which has `inside` from m0 on.  No
+  // branch depends on a lane: rows and columns outside C go out of range.
   __device__ __forceinline__ void rows(const lds_u8* block, int m0, int inside) {
     const int count = min(R, inside);  // a pass may reach past a block of 16 rows
+    if (count <= 0) return;
     // the wave's own sums, in LDS in the order of its instructions
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -346,17 +354,15 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
       const int r0 = lane / LPR + u0 * RP;
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
-        if (r0 + u * RP < count && left > 0) load_inputs(m0 + r0 + u * RP, res[u], aux[u]);
+        load_inputs(r0 + u * RP < count && left > 0, m0 + r0 + u * RP, res[u], aux[u]);
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         const int r = r0 + u * RP;
-        if (r < count && left > 0) {
-          const lds_u8* at = block + r * PITCH + (lane % LPR) * 32;
-          const f32x4 lo = *(const __attribute__((address_space(3))) f32x4*)at;
-          const f32x4 hi = *(const __attribute__((address_space(3))) f32x4*)(at + 16);
-          float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-          finish(m0 + r, x, res[u], aux[u]);
-        }
+        const lds_u8* p = block + (PASSES * RP > R ? min(r, R - 1) : r) * PITCH + (lane % LPR) * 32;
+        const f32x4 lo = *(const __attribute__((address_space(3))) f32x4*)p;
+        const f32x4 hi = *(const __attribute__((address_space(3))) f32x4*)(p + 16);
+        float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        finish(r < count && left > 0, m0 + r, x, res[u], aux[u]);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next block's sums
@@ -412,7 +418,7 @@ __global__ void __launch_bounds__(256) split_reduce_ep(KLaunch L, KEpis E) {
     x.columns(n0);
     if (row < M && x.left > 0) {
       Row8<DT> res, aux;
-      x.load_inputs(row, res, aux);
+      x.load_inputs(true, row, res, aux);
       const float* P = p.ws + (size_t)item * S * plane + (size_t)row * N + x.col;
       float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
       if ((N & 3) == 0 && x.left >= 8) {  // 16-byte aligned rows of the planes
@@ -428,7 +434,7 @@ __global__ void __launch_bounds__(256) split_reduce_ep(KLaunch L, KEpis E) {
           if (q < x.left)
             for (int s = 0; s < S; ++s) v[q] += P[s * plane + q];
       }
-      x.finish(row, v, res, aux);
+      x.finish(true, row, v, res, aux);
     }
     if (x.o.part) {
       x.put_sums((lds_u8*)smem, tid / Wave::LPR, BN, (tid % Wave::LPR) * 8);

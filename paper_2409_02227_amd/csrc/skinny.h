@@ -140,7 +140,7 @@ template <int DT, int TB> struct Skinny {
       part = x.o.part;
       if (row < m && x.left > 0) {
         Row8<DT> res, aux;
-        x.load_inputs(row, res, aux);
+        x.load_inputs(true, row, res, aux);
         const lds_u8* at = smem + row * PITCH + (tid % Epi::LPR) * 32;
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
 #pragma unroll
@@ -149,7 +149,7 @@ template <int DT, int TB> struct Skinny {
           hi += *(const lds_f32x4*)(at + w * (BM * PITCH) + 16);
         }
         float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        x.finish(row, v, res, aux);
+        x.finish(true, row, v, res, aux);
       }
       if (part) x.put_sums(smem + TABLE, row, BN, (tid % Epi::LPR) * 8);
     }
