@@ -249,6 +249,8 @@ const void* skinny_ep(int dt, int tb);
 constexpr int skinny_cols(int tb) { return tb ? 16 : 64; }
 constexpr int skinny_kstep(int es) { return es == 1 ? 128 : 64; }
 constexpr int skinny_ahead(int es, int tb) { return tb && es != 1 ? 8 : 4; }
+// Grouped products over rows in tiles of kSkinnyRows rows (skinny.h).
+GroupKernel group_few(int dt, int tb);
 GroupKernel group_bf16(int over_k, int tb, int tile);
 GroupKernel group_f16(int over_k, int tb, int tile);
 GroupKernel group_fp8(int over_k, int tb, int tile);

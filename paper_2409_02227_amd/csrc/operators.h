@@ -321,6 +321,32 @@ const GroupTileCost& group_rows_tile(const gdy_ctx* ctx, const gdy_grouped& g, b
   return *best;
 }
 
+// Whether a product over rows runs in tiles of 16 rows with K over a workgroup's waves
+// (skinny.h).  Few workgroups wait for one K tile after another (32 x 64 tiles: 0.22 to 0.42 us
+// each); these wait for a round of loads, 2 to 4 KiB of a row, in 2.5 us (K x N of 16-bit
+// types, whose loads are 8 bytes, 3.6, and 1.3 TB/s of weights in place of 4), but
+// read a group's B once for 16 rows, from L2 at 8 TB/s.  us, 32 x 64 tiles and these: bf16 nt
+// 65 rows, 768 x 4096 20.7 and 11.0; 2 rows of 128 groups, 4096 x 4096 21.2 and 10.3; 64
+// rows, 4096 x 4096 20.7 and 32.2; nn 2 rows of 16 groups, 72 x 4096 20.8 and 12.2, a row,
+// 4096 x 14336 62.4 and 88.5; fp32 nn 65 rows, 768 x 4096 58.8 and 29.3; fp8 nt 64 rows in
+// 16 groups, 2048 x 2048 13.2 and 21.2, 16 rows in 4, 256 x 16384 34.6 and 14.5.
+bool group_rows_few(const gdy_grouped& g, bool copies) {
+  if (!copies || g.k == 0 || !group_few(g.a_type, g.trans_b).func) return false;
+  const int es = elem_size(g.a_type);
+  const bool narrow = es == 2 && !g.trans_b;
+  const double groups = (double)std::min<int64_t>(g.groups, g.rows), avg = (double)g.rows / groups;
+  const double slots = groups <= 1 ? std::ceil((double)g.rows / kSkinnyRows)
+                                   : groups / (1.0 - std::exp(-kSkinnyRows / avg));  // as group_rows_tile
+  const double kbytes = (double)g.k * es, cols = skinny_cols(g.trans_b);
+  const double read = slots * std::ceil(g.n / cols) * (cols + std::min<double>(kSkinnyRows, g.rows / slots)) * kbytes;
+  const double rounds = std::ceil(kbytes / (8.0 * skinny_kstep(es) * skinny_ahead(es, g.trans_b)));
+  const double weights = groups * g.n * kbytes;
+  double few = std::max(rounds * (narrow ? 3.6 : 2.5), read / 8e6);
+  double tiles = std::ceil(kbytes / 128) * (es == 4 ? 0.42 : es == 2 ? 0.25 : 0.22);
+  if (narrow) few = std::max(few, weights / 1.3e6), tiles = std::max(tiles, weights / 4e6);
+  return few < tiles;
+}
+
 // The kernel of a product over K.
 int group_k_tile(const gdy_ctx* ctx, const gdy_grouped& g, bool copies) {
   auto tiles = [&](int64_t b) { return (g.k + b - 1) / b * ((g.n + b - 1) / b) * g.groups; };
@@ -368,9 +394,11 @@ gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue
   a.c_vec = vec(g.c, g.ldc, g.stride_c);
   const bool copies = a.a_dma && a.b_dma;
   const GroupTileCost* rows_tile = over_k ? nullptr : &group_rows_tile(ctx, g, copies);
+  const bool few = !over_k && group_rows_few(g, copies);
   const GroupKernel kern =
-      group_kernel_of(g.a_type, over_k, g.trans_b, over_k ? group_k_tile(ctx, g, copies) : rows_tile->tile);
-  a.bm = over_k ? kern.bm : rows_tile->bm;
+      few ? group_few(g.a_type, g.trans_b)
+          : group_kernel_of(g.a_type, over_k, g.trans_b, over_k ? group_k_tile(ctx, g, copies) : rows_tile->tile);
+  a.bm = over_k || few ? kern.bm : rows_tile->bm;
   a.max_slots = (int32_t)max_row_tiles(g.rows, g.groups, a.bm);
   a.xcd_cus = std::max(ctx->cus / kXcds, 1);
   const int sums_per_tile = !over_k && a.bm == 256 ? 2 : 1;

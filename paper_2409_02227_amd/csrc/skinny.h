@@ -14,6 +14,10 @@
 // round, 14-16 and 9-15 us; K = 8192, four, 14-37 and 14-42; K x N, K = 2048, two, 14-17 and 9-14;
 // K = 8192, eight, 16-38 and 26-47; fp8 N x K, K = 8192, two, 14-25 and 9-22).
 //
+// Grouped products over rows take the same loop (grouped_few), for any K and row count
+// where 32 x 64 tiles would wait for one K tile after another: their sums have no split
+// otherwise.
+//
 // Fragments (lane l, i = l % 16, g = l / 16; A's and B's K agree):
 //  * N x K: lane l holds 16 bytes of K of column i, as A's of row i: K bytes 64 step +
 //    16 g (8-bit types: 32 bytes, 128 step + 32 g).
@@ -22,6 +26,7 @@
 //    rows of 16 bytes, no transpose); MFMA j takes column 4i + j of every lane.
 #pragma once
 #include "go_kernel_ep.h"
+#include "grouped.h"
 
 namespace gdy {
 
@@ -171,6 +176,39 @@ template <int DT, int TB>
 __global__ void __launch_bounds__(512) go_skinny(KLaunch L, KEpis) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[Skinny<DT, TB>::LDS];
   ep_member<512, Skinny<DT, TB>>(L, (lds_u8*)smem);
+}
+
+// Products grouped by expert over rows, 16 rows a tile, K of any length: a round of loads
+// after the other.
+template <int DT, int TB>
+__global__ void __launch_bounds__(512) grouped_few(KGroup g) {
+  typedef Skinny<DT, TB> T;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDS];
+  constexpr int ES = ElemSize<DT>::v;
+  const int tn = (g.n + T::BN - 1) / T::BN;
+  const int total = total_slots(g.offsets, g.groups, g.rows, T::BM, g.max_slots) * tn;
+  const int per = (total + kXcds - 1) / kXcds;
+  const int j = (int)blockIdx.x / kXcds, id = ((int)blockIdx.x & (kXcds - 1)) * per + j;
+  if (j >= per || id >= total) return;
+  GroupSlot s;
+  if (!find_slot(g.offsets, g.groups, g.rows, T::BM, id / tn, s)) return;
+  int ti, tj;
+  group_tile(id - s.first * tn, (s.count + T::BM - 1) / T::BM, tn, ti, tj);
+  GroupEpi e;
+  e.e = uniform(s.e), e.row = uniform(s.lo + ti * T::BM), e.n0 = uniform(tj * T::BN);
+  e.m = uniform(min(T::BM, s.count - ti * T::BM)), e.n = uniform(min(T::BN, g.n - tj * T::BN));
+  e.slot = uniform(s.first + ti), e.os = OutSize<DT>::v, e.over_k = false;
+  const uint8_t* a = g.a + (int64_t)e.row * g.lda * ES;
+  const uint8_t* b = g.b + e.e * g.stride_b + (TB == 1 ? (int64_t)e.n0 * g.ldb : (int64_t)e.n0) * ES;
+  T::tile(a, b, g.lda * ES, g.ldb * ES, e.m, e.n, g.k, e, 0, 0, (lds_u8*)smem);
+}
+
+template <int DT> GroupKernel few_kernel(int tb) {
+  if (tb)
+    return GroupKernel{reinterpret_cast<const void*>(&grouped_few<DT, 1>), kSkinnyRows, Skinny<DT, 1>::BN, 512};
+  if constexpr (DT != DT_FP8)
+    return GroupKernel{reinterpret_cast<const void*>(&grouped_few<DT, 0>), kSkinnyRows, Skinny<DT, 0>::BN, 512};
+  else return GroupKernel{nullptr, 0, 0, 0};
 }
 
 template <int DT> const void* skinny_kernel(int tb) {

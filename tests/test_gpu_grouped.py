@@ -128,6 +128,20 @@ def test_rows_backward(ctx, dtype, rows, offsets):
                       sums="groups"))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "fp8", "f32"])
+@pytest.mark.parametrize("rows,offsets,n,k", [(1, [0, 0, 1], 112, 2592), (65, [0, 65], 72, 4096),
+                                              (40, [3, 20, 20, 33], 200, 4096), (100, [0, 16, 33, 34, 90], 136, 8192),
+                                              (17, [0, 17], 16, 4112), (300, [0, 40, 290, 290, 300], 24, 4096)])
+@pytest.mark.parametrize("tb", [0, 1])
+def test_rows_of_a_long_k(ctx, dtype, rows, offsets, n, k, tb):
+    """Few rows and columns and a long K, on tiles of 16 rows where operands are aligned."""
+    q = rows + n + tb
+    run(ctx, Rows(dtype, rows, offsets, n, k, tb, ACTS[q % 5], bias="groups", residual=True, aux=True, sums="groups",
+                  scales=dtype == "fp8", pad=(0, 16)[tb]))
+    run(ctx, Rows(dtype, rows, offsets, n, k, tb, ACTS[(q + 1) % 5], grad=True, sums="shared", seed=1))
+    run(ctx, Rows(dtype, rows, offsets, n, k, tb, bias="shared", seed=2))
+
+
 def test_many_groups(ctx):
     """More groups than a wave has lanes, and the largest number."""
     gen = torch.Generator().manual_seed(5)
