@@ -200,16 +200,17 @@ __global__ void __launch_bounds__(T::NT) grouped_rows(KGroup g) {
   T::run(tile_args<DT, 0, TB>(g, a, b, e.m, e.n, g.k), (lds_u8*)smem, e);
 }
 
-// Over K.  A group's tiles are dealt to the XCDs in contiguous runs.
+// Over K.  Every group's tiles are dealt to all XCDs, each a contiguous run of them, with no
+// workgroup left idle: a 256 x 256 one would hold a CU (128 groups of 64 rows, 512 x 256, two
+// tiles each: 38.6 us where each group took eight workgroups, now 16.2).
 template <int DT, class T>
 __global__ void __launch_bounds__(T::NT) grouped_k(KGroup g) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDS];
   constexpr int ES = ElemSize<DT>::v;
   const int tm = (g.m + T::BM - 1) / T::BM, tn = (g.n + T::BN - 1) / T::BN;
-  const int per = (tm * tn + kXcds - 1) / kXcds;
-  const int group = (int)blockIdx.x / (per * kXcds), r = (int)blockIdx.x - group * (per * kXcds);
-  const int t = (r & (kXcds - 1)) * per + r / kXcds;
-  if (t >= tm * tn) return;
+  const int tiles = tm * tn, group = (int)blockIdx.x / tiles, r = (int)blockIdx.x - group * tiles;
+  const int x = r & (kXcds - 1);
+  const int t = x * (tiles / kXcds) + min(x, tiles & (kXcds - 1)) + r / kXcds;
   const GroupRows rows = group_rows(g.offsets, g.groups, g.rows, group);
   int ti, tj;
   group_tile(t, tm, tn, ti, tj);

@@ -347,11 +347,16 @@ bool group_rows_few(const gdy_grouped& g, bool copies) {
   return few < tiles;
 }
 
-// The kernel of a product over K.
+// The kernel of a product over K: 256 x 256 tiles where they give most CUs one, 128 x 128
+// ones where every CU has more than one.  us on 256, 128 and 64 (bf16, 8192 rows, tiles of 256): 16
+// groups of 512 x 1024, 128 tiles, 25.2, 19.9 and 25.5; 32 groups, 256 tiles, 22.6, 24.7 and
+// 33.2; one group of 4096 x 2048, 157, 138 and 286, 4096 x 4096 197, 272 and 624; 4 groups, 4096
+// rows, 512 x 512, 16 tiles, 30.5, 19.2 and 10.6, 1024 x 1024, 64 tiles, 31.5, 22.0 and 20.8; fp32 8
+// groups, 4096 rows, 2048 x 1024, 256 tiles, 148 on 128 and 166 on 64.
 int group_k_tile(const gdy_ctx* ctx, const gdy_grouped& g, bool copies) {
   auto tiles = [&](int64_t b) { return (g.k + b - 1) / b * ((g.n + b - 1) / b) * g.groups; };
-  if (copies && g.a_type != GDY_F32 && tiles(256) >= ctx->cus / 2) return 0;
-  return tiles(128) >= ctx->cus / 2 ? 1 : 2;
+  if (copies && g.a_type != GDY_F32 && 4 * tiles(256) >= 3 * ctx->cus) return 0;
+  return tiles(128) > ctx->cus ? 1 : 2;
 }
 
 gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue* ep, hipStream_t hs) {
@@ -424,7 +429,7 @@ gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue
     a.epi.part = ctx->split_ws;
   }
   const int64_t tn = (g.n + kern.bn - 1) / kern.bn;
-  const int64_t grid = over_k ? (((m + kern.bm - 1) / kern.bm * tn + kXcds - 1) / kXcds) * kXcds * g.groups
+  const int64_t grid = over_k ? (m + kern.bm - 1) / kern.bm * tn * g.groups
                               : (((int64_t)a.max_slots * tn + kXcds - 1) / kXcds + a.xcd_cus / 2) * kXcds;
   if (grid * kern.threads > UINT32_MAX)  // threads of a launch
     return fail(ctx, GDY_ERR_UNSUPPORTED, "grouped: a grid of %lld workgroups", (long long)grid);
