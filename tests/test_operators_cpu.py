@@ -309,9 +309,8 @@ def test_null_arguments(ctx):
 
 
 # ---- the kernels' code -------------------------------------------------------------
-@pytest.mark.parametrize("unit", [f"kernels_{f}_{dt}" for f in ("ep", "ep1", "group") for dt in ("bf16", "f16", "fp8", "f32")])
-def test_wait_states_and_no_scratch(tmp_path, unit):
-    """As test_copy_wait_states, for the kernels of epilogues and grouped products."""
+def device_code(tmp_path, unit):
+    """(disassembly, notes) of a unit's device code."""
     obj = os.path.join(waits.BUILD, unit + ".o")
     tools = [os.path.join(waits.LLVM, t) for t in ("llvm-objcopy", "clang-offload-bundler", "llvm-objdump", "llvm-readelf")]
     if not os.path.exists(obj) or not all(shutil.which(t) for t in tools):
@@ -320,9 +319,25 @@ def test_wait_states_and_no_scratch(tmp_path, unit):
     subprocess.run([tools[0], f"--dump-section=.hip_fatbin={fat}", obj, os.devnull], check=True)
     subprocess.run([tools[1], "--unbundle", "--type=o", f"--input={fat}", f"--output={dev}",
                     "--targets=hipv4-amdgcn-amd-amdhsa--gfx950"], check=True)
-    text = subprocess.run([tools[2], "-d", "--no-show-raw-insn", dev], check=True, capture_output=True, text=True).stdout
-    assert waits.check_copies(text) > 50
+    return [subprocess.run([tools[q], *args, dev], check=True, capture_output=True, text=True).stdout
+            for q, args in ((2, ["-d", "--no-show-raw-insn"]), (3, ["--notes"]))]
+
+
+def check_code(unit, text, notes):
     assert not re.search(r"\bv_pk_(add|mul|fma)_f32\b", text)
-    notes = subprocess.run([tools[3], "--notes", dev], check=True, capture_output=True, text=True).stdout
     scratch = [int(x) for x in re.findall(r"\.private_segment_fixed_size:\s*(\d+)", notes)]
     assert len(scratch) > 0 and set(scratch) == {0}, (unit, scratch)
+
+
+@pytest.mark.parametrize("unit", [f"kernels_{f}_{dt}" for f in ("ep", "ep1", "group") for dt in ("bf16", "f16", "fp8", "f32")])
+def test_wait_states_and_no_scratch(tmp_path, unit):
+    """As test_copy_wait_states, for the kernels of epilogues and grouped products."""
+    text, notes = device_code(tmp_path, unit)
+    assert waits.check_copies(text) > 50
+    check_code(unit, text, notes)
+
+
+@pytest.mark.parametrize("unit", ["kernels_skinny", "kernels_act"])
+def test_no_scratch(tmp_path, unit):
+    """The kernels of few rows and of activation gradients, which copy nothing to LDS."""
+    check_code(unit, *device_code(tmp_path, unit))
