@@ -535,11 +535,11 @@ struct Extent {
   uintptr_t lo, hi;  // [lo, hi) in bytes; empty when lo == hi
 };
 
+// The bytes of a stored matrix; false where a kernel's offsets could not hold them.
 bool stored_extent(int64_t rows, int64_t cols, int64_t ld, int es, int64_t* bytes) {
-  if (rows == 0 || cols == 0) {
-    *bytes = 0;
-    return true;
-  }
+  *bytes = 0;
+  if (rows == 0 || cols == 0) return true;
+  if (rows > INT32_MAX || cols > INT32_MAX || ld > INT32_MAX) return false;  // the products below hold
   *bytes = ((rows - 1) * ld + cols) * es;
   // the kernels form 32-bit byte offsets up to 256 rows past the edge
   return (rows + 256) * ld * es + 1024 < (int64_t)INT32_MAX;

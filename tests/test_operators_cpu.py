@@ -301,6 +301,30 @@ def test_act_grad_checks(ctx, g, want):
     assert status(ctx, ctx.lib.gdy_execute_act_grad, ctypes.byref(act_grad(**g)), None) == want
 
 
+@pytest.mark.parametrize("ld", [(1 << 31) - 1, 1 << 55, (1 << 55) + 96, 1 << 61, 1 << 62, (1 << 62) + 96, (1 << 63) - 1])
+def test_leading_dimensions_past_every_offset(ctx, ld):
+    """Pitches whose product with rows and element size leaves 64 bits, and the largest of 32, are refused as
+    the ones just past the limit are."""
+    for e in ({"ldr": ld}, {"ldaux": ld}):
+        assert run_epilogue(ctx, [gemm()], [epilogue(**e)]) == UNSUPPORTED
+        assert run_epilogue(ctx, [gemm(m=1)], [epilogue(**e)]) == UNSUPPORTED
+        assert status(ctx, ctx.lib.gdy_execute_grouped, ctypes.byref(grouped()), ctypes.byref(epilogue(**e)), None) == UNSUPPORTED
+    for g in ({"lda": ld}, {"ldb": ld}, {"ldc": ld}):
+        assert run_epilogue(ctx, [gemm(**g)], [gdy.EpilogueDesc()]) == UNSUPPORTED
+        assert status(ctx, ctx.lib.gdy_execute, (gdy.GemmDesc * 1)(gemm(**g)), 1, gdy.SELECTOR, 0, None, None) == UNSUPPORTED
+        add = gemm(op=gdy.ADD, k=0, lda=96, **{k: v for k, v in g.items() if k != "lda"})
+        add.lda = g.get("lda", 96)
+        assert status(ctx, ctx.lib.gdy_execute, (gdy.GemmDesc * 1)(add), 1, gdy.SELECTOR, 0, None, None) == UNSUPPORTED
+        for over in (0, 1):
+            assert status(ctx, ctx.lib.gdy_execute_grouped, ctypes.byref(grouped(over=over, **g)), None, None) == UNSUPPORTED
+    for a in ({"lddy": ld}, {"ldz": ld}, {"lddz": ld}):
+        assert status(ctx, ctx.lib.gdy_execute_act_grad, ctypes.byref(act_grad(**a)), None) == UNSUPPORTED
+    # rows and columns past 32 bits
+    assert run_epilogue(ctx, [gemm(m=ld, trans_a=1, lda=ld, ldc=96)], [gdy.EpilogueDesc()]) == UNSUPPORTED
+    assert run_epilogue(ctx, [gemm(n=ld, ldb=ld, ldc=ld)], [gdy.EpilogueDesc()]) == UNSUPPORTED
+    assert run_epilogue(ctx, [gemm(k=ld, lda=ld)], [gdy.EpilogueDesc()]) == UNSUPPORTED
+
+
 def test_null_arguments(ctx):
     assert ctx.lib.gdy_execute_grouped(None, None, None, None) == INVALID
     assert ctx.lib.gdy_execute_grouped(ctx.h, None, None, None) == INVALID
