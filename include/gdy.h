@@ -138,7 +138,7 @@ typedef struct {
    * C + b*stride_c (strides in elements).  batch 0 or 1: a single GEMM and
    * the strides are ignored.  C items must not overlap each other; A and B
    * items may (stride 0 broadcasts one operand).  Every item obeys the
-   * single-GEMM extent limits. */
+   * single-GEMM extent limits; strides are at most 2^44. */
   int32_t batch;
   int32_t op;                       /* gdy_op: what this entry computes (0: a GEMM)         */
   int64_t stride_a, stride_b, stride_c;

@@ -545,6 +545,17 @@ bool stored_extent(int64_t rows, int64_t cols, int64_t ld, int es, int64_t* byte
   return (rows + 256) * ld * es + 1024 < (int64_t)INT32_MAX;
 }
 
+// The matrix rows x cols at p, `items` of them `stride` elements apart.
+Extent matrix_range(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t items, int64_t stride, int es) {
+  if (!p || rows <= 0 || cols <= 0 || items <= 0) return Extent{0, 0};
+  const uintptr_t lo = (uintptr_t)p;
+  const __int128 bytes = ((__int128)(items - 1) * stride + (__int128)(rows - 1) * ld + cols) * es;
+  return Extent{lo, bytes > (__int128)(UINTPTR_MAX - lo) ? UINTPTR_MAX : lo + (uintptr_t)bytes};
+}
+
+// Strides between items in elements, far inside what 64-bit byte offsets hold.
+const int64_t kMaxStride = (int64_t)1 << 44;
+
 // The element-wise add: A, B and C are M x N regions of one type.
 gdy_status validate_add(gdy_ctx* ctx, const gdy_gemm& g, int i, Extent* ea, Extent* eb, Extent* ec) {
   const bool t = g.a_type == g.b_type && g.a_type == g.c_type &&
@@ -567,12 +578,9 @@ gdy_status validate_add(gdy_ctx* ctx, const gdy_gemm& g, int i, Extent* ea, Exte
     return fail(ctx, GDY_ERR_UNSUPPORTED, "add %d: extent too large", i);
   if (nb > 1 && g.stride_c * es < cb)
     return fail(ctx, GDY_ERR_ALIAS, "add %d: batch items of C overlap (stride_c too small)", i);
-  ea->lo = (uintptr_t)g.a;
-  ea->hi = ea->lo + (uintptr_t)((nb - 1) * g.stride_a * es + ab);
-  eb->lo = (uintptr_t)g.b;
-  eb->hi = eb->lo + (uintptr_t)((nb - 1) * g.stride_b * es + bb);
-  ec->lo = (uintptr_t)g.c;
-  ec->hi = ec->lo + (uintptr_t)((nb - 1) * g.stride_c * es + cb);
+  *ea = matrix_range(g.a, g.m, g.n, g.lda, nb, nb > 1 ? g.stride_a : 0, es);
+  *eb = matrix_range(g.b, g.m, g.n, g.ldb, nb, nb > 1 ? g.stride_b : 0, es);
+  *ec = matrix_range(g.c, g.m, g.n, g.ldc, nb, nb > 1 ? g.stride_c : 0, es);
   return GDY_OK;
 }
 
@@ -586,6 +594,8 @@ gdy_status validate_one(gdy_ctx* ctx, const gdy_gemm& g, int i, Extent* ea, Exte
   if (g.batch < 0) return fail(ctx, GDY_ERR_INVALID_ARG, "gemm %d: negative batch", i);
   if (g.batch > 1 && (g.stride_a < 0 || g.stride_b < 0 || g.stride_c < 0))
     return fail(ctx, GDY_ERR_INVALID_ARG, "gemm %d: negative batch stride", i);
+  if (g.batch > 1 && std::max({g.stride_a, g.stride_b, g.stride_c}) > kMaxStride)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "gemm %d: batch stride too large", i);
   if (g.op == GDY_OP_ADD) return validate_add(ctx, g, i, ea, eb, ec);
   const bool t16 = (g.a_type == GDY_F16 && g.b_type == GDY_F16 && g.c_type == GDY_F16) ||
                    (g.a_type == GDY_BF16 && g.b_type == GDY_BF16 && g.c_type == GDY_BF16);
@@ -618,8 +628,7 @@ gdy_status validate_one(gdy_ctx* ctx, const gdy_gemm& g, int i, Extent* ea, Exte
     if (bm * bn * nb >= (int64_t)INT32_MAX)
       return fail(ctx, GDY_ERR_UNSUPPORTED, "gemm %d: batch x tiles too large", i);
   }
-  ec->lo = (uintptr_t)g.c;
-  ec->hi = ec->lo + (uintptr_t)((nb - 1) * g.stride_c * os + cb);
+  *ec = matrix_range(g.c, g.m, g.n, g.ldc, nb, nb > 1 ? g.stride_c : 0, os);
   if (g.k == 0) return GDY_OK;
   if (!g.a || !g.b) return fail(ctx, GDY_ERR_INVALID_ARG, "gemm %d: null A or B", i);
   if (g.lda < (g.trans_a ? g.m : g.k)) return fail(ctx, GDY_ERR_INVALID_ARG, "gemm %d: lda too small", i);
@@ -630,10 +639,8 @@ gdy_status validate_one(gdy_ctx* ctx, const gdy_gemm& g, int i, Extent* ea, Exte
   const bool oka = g.trans_a ? stored_extent(g.k, g.m, g.lda, es, &ab) : stored_extent(g.m, g.k, g.lda, es, &ab);
   const bool okb = g.trans_b ? stored_extent(g.n, g.k, g.ldb, es, &bb) : stored_extent(g.k, g.n, g.ldb, es, &bb);
   if (!oka || !okb) return fail(ctx, GDY_ERR_UNSUPPORTED, "gemm %d: A or B extent too large", i);
-  ea->lo = (uintptr_t)g.a;
-  ea->hi = ea->lo + (uintptr_t)((nb - 1) * g.stride_a * es + ab);
-  eb->lo = (uintptr_t)g.b;
-  eb->hi = eb->lo + (uintptr_t)((nb - 1) * g.stride_b * es + bb);
+  *ea = matrix_range(g.a, g.trans_a ? g.k : g.m, g.trans_a ? g.m : g.k, g.lda, nb, nb > 1 ? g.stride_a : 0, es);
+  *eb = matrix_range(g.b, g.trans_b ? g.n : g.k, g.trans_b ? g.k : g.n, g.ldb, nb, nb > 1 ? g.stride_b : 0, es);
   return GDY_OK;
 }
 

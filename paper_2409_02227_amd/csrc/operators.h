@@ -15,17 +15,6 @@ struct Range {
   int twin;  // ranges of one nonzero twin may coincide
 };
 
-// The matrix rows x cols at p, `items` of them `stride` elements apart.
-Extent matrix_range(const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t items, int64_t stride, int es) {
-  if (!p || rows <= 0 || cols <= 0 || items <= 0) return Extent{0, 0};
-  const uintptr_t lo = (uintptr_t)p;
-  const __int128 bytes = ((__int128)(items - 1) * stride + (__int128)(rows - 1) * ld + cols) * es;
-  return Extent{lo, bytes > (__int128)(UINTPTR_MAX - lo) ? UINTPTR_MAX : lo + (uintptr_t)bytes};
-}
-
-// Strides between items in elements, far inside what 64-bit byte offsets hold.
-const int64_t kMaxStride = (int64_t)1 << 44;
-
 // Values of a bias_grad: sums of 2^26 columns, of all members of a submission, are one
 // launch of fewer than 2^32 threads.
 const int64_t kMaxBiasGrad = (int64_t)1 << 26;

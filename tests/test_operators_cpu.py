@@ -325,6 +325,28 @@ def test_leading_dimensions_past_every_offset(ctx, ld):
     assert run_epilogue(ctx, [gemm(k=ld, lda=ld)], [gdy.EpilogueDesc()]) == UNSUPPORTED
 
 
+@pytest.mark.parametrize("stride", [1 << 45, 1 << 61, (1 << 61) + 64 * 128, 1 << 62, (1 << 63) - 1])
+def test_batch_strides_past_every_offset(ctx, stride):
+    """Strides between a member's items that leave 64-bit byte offsets are refused, as an epilogue's are; the
+    largest allowed ones with the most items still compare as ranges."""
+    good = {"batch": 3, "stride_a": 64 * 128, "stride_b": 128 * 96, "stride_c": 64 * 96}
+    zero = gdy.EpilogueDesc()
+    for field in ("stride_a", "stride_b", "stride_c"):
+        g = gemm(**dict(good, **{field: stride}))
+        add = gemm(**dict(good, **{field: stride}), op=gdy.ADD, k=0, lda=96)
+        for x in (g, add):
+            assert run_epilogue(ctx, [x], [zero]) == UNSUPPORTED
+            assert status(ctx, ctx.lib.gdy_execute, (gdy.GemmDesc * 1)(x), 1, gdy.SELECTOR, 0, None, None) == UNSUPPORTED
+        single = gemm(**{field: stride})  # ignored without a batch
+        assert run_epilogue(ctx, [single], [zero]) == OK
+    far = {"stride_a": 1 << 44, "a": 1 << 46, "batch": 3, "stride_c": 64 * 96, "stride_b": 0}
+    assert run_epilogue(ctx, [gemm(**far)], [zero]) == OK
+    most = {"m": 1, "n": 1, "k": 1, "lda": 1, "ldb": 1, "ldc": 1, "batch": (1 << 31) - 2, "stride_a": 1 << 44, "a": 8 << 40}
+    assert run_epilogue(ctx, [gemm(**dict(most, stride_c=1))], [zero]) == OK
+    # (C behind A's start: inside what A's items span)
+    assert run_epilogue(ctx, [gemm(**dict(most, stride_c=1, c=9 << 40))], [zero]) == ALIAS
+
+
 def test_null_arguments(ctx):
     assert ctx.lib.gdy_execute_grouped(None, None, None, None) == INVALID
     assert ctx.lib.gdy_execute_grouped(ctx.h, None, None, None) == INVALID
