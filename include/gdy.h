@@ -337,7 +337,7 @@ typedef struct {
   int32_t reserved;                 /* must be 0                                            */
   const void* residual; int64_t ldr;    /* R: M x N of C's type, or NULL; ldr >= n          */
   void* aux;            int64_t ldaux;  /* M x N of C's type, or NULL; ldaux >= n           */
-  float* bias_grad;                 /* N values, or NULL; overwritten; at most 2^26 in all   */
+  float* bias_grad;                 /* N values, or NULL; overwritten; at most 2^26 an entry  */
   /* between items of a strided batch (or groups, gdy_execute_grouped), in elements: bias 0
    * shares one bias, bias_grad 0 adds the items' sums up.  Ignored for a single GEMM. */
   int64_t stride_bias, stride_r, stride_aux, stride_bias_grad;

@@ -39,15 +39,19 @@ __device__ __forceinline__ void column_sums(const float* part, float* out, int n
   }
 }
 
+// One work item a workgroup, more where a grid of one each would pass 2^32 threads.
 template <int COLS, int LANES>
 __global__ void __launch_bounds__(COLS * LANES) bias_sums(BiasSums s) {
   __shared__ float lds[COLS * LANES];
-  int u = 0;
-  while (u + 1 < s.count && (int)blockIdx.x >= s.first[u + 1]) ++u;
-  const int blocks = (s.n[u] + COLS - 1) / COLS, b = (int)blockIdx.x - s.first[u];
-  const int item = b / blocks;
-  column_sums<COLS, LANES>(s.part[u] + (int64_t)item * s.rows[u] * s.n[u], s.out[u] + item * s.stride[u], s.n[u],
-                           s.rows[u], (b - item * blocks) * COLS, lds);
+  for (int w = (int)blockIdx.x; w < s.first[s.count]; w += (int)gridDim.x) {
+    if (w != (int)blockIdx.x) __syncthreads();  // the item before has read the sums
+    int u = 0;
+    while (u + 1 < s.count && w >= s.first[u + 1]) ++u;
+    const int blocks = (s.n[u] + COLS - 1) / COLS, b = w - s.first[u];
+    const int item = b / blocks;
+    column_sums<COLS, LANES>(s.part[u] + (int64_t)item * s.rows[u] * s.n[u], s.out[u] + item * s.stride[u], s.n[u],
+                             s.rows[u], (b - item * blocks) * COLS, lds);
+  }
 }
 
 // The sums of group e, or of all groups (GroupSums::shared).

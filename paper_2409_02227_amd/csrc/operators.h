@@ -15,8 +15,8 @@ struct Range {
   int twin;  // ranges of one nonzero twin may coincide
 };
 
-// Values of a bias_grad: sums of 2^26 columns, of all members of a submission, are one
-// launch of fewer than 2^32 threads.
+// Values of a member's bias_grad, all items together: the work items of a launch of
+// kMaxFused members' sums, at most one a value, are a 31-bit count.
 const int64_t kMaxBiasGrad = (int64_t)1 << 26;
 
 gdy_status check_ranges(gdy_ctx* ctx, const std::vector<Range>& r) {
@@ -146,9 +146,10 @@ hipError_t launch_bias_sums(BiasSums* s, hipStream_t hs, hipEvent_t stop) {
     wg += items * ((s->n[u] + cols - 1) / cols);
   }
   s->first[s->count] = wg;
+  const int threads = sum_threads(s->many != 0);
+  const int grid = (int)std::min<int64_t>(wg, UINT32_MAX / threads);
   void* argv[] = {s};
-  return hipExtLaunchKernel(bias_sum_kernel(s->many != 0), dim3(wg), dim3(sum_threads(s->many != 0)), argv, 0, hs,
-                            nullptr, stop, 0);
+  return hipExtLaunchKernel(bias_sum_kernel(s->many != 0), dim3(grid), dim3(threads), argv, 0, hs, nullptr, stop, 0);
 }
 
 hipError_t launch_group_sums(const GroupSums& s, hipStream_t hs) {
