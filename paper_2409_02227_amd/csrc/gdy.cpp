@@ -556,6 +556,11 @@ Extent matrix_range(const void* p, int64_t rows, int64_t cols, int64_t ld, int64
 // Strides between items in elements, far inside what 64-bit byte offsets hold.
 const int64_t kMaxStride = (int64_t)1 << 44;
 
+// Workgroups of a launch: the runtime takes fewer than 2^32 threads, 512 a workgroup
+// at most.  Members of more work items get fewer workgroups, which go on to further
+// items by a 31-bit index: kMaxItems and a grid's workgroups do not pass it.
+const int64_t kMaxGrid = UINT32_MAX / 512, kMaxItems = INT32_MAX - kMaxGrid;
+
 // The element-wise add: A, B and C are M x N regions of one type.
 gdy_status validate_add(gdy_ctx* ctx, const gdy_gemm& g, int i, Extent* ea, Extent* eb, Extent* ec) {
   const bool t = g.a_type == g.b_type && g.a_type == g.c_type &&
@@ -576,6 +581,8 @@ gdy_status validate_add(gdy_ctx* ctx, const gdy_gemm& g, int i, Extent* ea, Exte
   if (!stored_extent(g.m, g.n, g.lda, es, &ab) || !stored_extent(g.m, g.n, g.ldb, es, &bb) ||
       !stored_extent(g.m, g.n, g.ldc, es, &cb))
     return fail(ctx, GDY_ERR_UNSUPPORTED, "add %d: extent too large", i);
+  if ((g.m + 31) / 32 * ((g.n + 127) / 128) * nb > kMaxItems)  // tiles (kEwRows x 512 bytes)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "add %d: batch x tiles too large", i);
   if (nb > 1 && g.stride_c * es < cb)
     return fail(ctx, GDY_ERR_ALIAS, "add %d: batch items of C overlap (stride_c too small)", i);
   *ea = matrix_range(g.a, g.m, g.n, g.lda, nb, nb > 1 ? g.stride_a : 0, es);
@@ -625,7 +632,7 @@ gdy_status validate_one(gdy_ctx* ctx, const gdy_gemm& g, int i, Extent* ea, Exte
     return fail(ctx, GDY_ERR_ALIAS, "gemm %d: batch items of C overlap (stride_c too small)", i);
   {
     const int64_t bm = (g.m + 15) / 16, bn = (g.n + 15) / 16;  // tiles of the smallest kernel
-    if (bm * bn * nb >= (int64_t)INT32_MAX)
+    if (bm * bn * nb > kMaxItems)
       return fail(ctx, GDY_ERR_UNSUPPORTED, "gemm %d: batch x tiles too large", i);
   }
   *ec = matrix_range(g.c, g.m, g.n, g.ldc, nb, nb > 1 ? g.stride_c : 0, os);
@@ -1397,6 +1404,9 @@ int few_tiles(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, int mo
   return deep ? 5 : low && unsplit ? 1 : 0;
 }
 
+// A member's share of a launch of `members`.
+int64_t max_span(int members) { return (kMaxGrid / std::max(members, 1)) & ~7LL; }
+
 // Workgroup ranges of one dispatch: each GEMM gets its own grid (tiles, or
 // its cap x occupancy), every range but the last rounded up to a multiple
 // of 8 so each GEMM starts on XCD 0 (the extra workgroups find no tile).  epilogues:
@@ -1439,7 +1449,9 @@ gdy_status build_launch(gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, in
       a.code = e.code;
     }
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n * a.batch;
-    const int64_t cap = v.cap > 0 ? (int64_t)v.cap * std::max(ctx->kernels[v.kernel].occupancy, 1) : INT32_MAX;
+    const int64_t most = max_span(L->count);
+    const int64_t cap =
+        v.cap > 0 ? std::min<int64_t>((int64_t)v.cap * std::max(ctx->kernels[v.kernel].occupancy, 1), most) : most;
     L->first[u] = (int32_t)wg;
     int64_t span = std::max<int64_t>(std::min(tiles, cap), 1);
     const int s = std::max(p.split_of[i], 1);
@@ -1456,7 +1468,6 @@ gdy_status build_launch(gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, in
     if (u + 1 < L->count) span = (span + 7) & ~7LL;
     wg += span;
   }
-  if (wg > INT32_MAX) return fail(ctx, GDY_ERR_UNSUPPORTED, "dispatch grid of %lld workgroups", (long long)wg);
   L->first[L->count] = (int32_t)wg;
   *grid = (int)wg;
   if (!*split && one_tile) place_xcds(ctx, g, p, members, L, grid);
@@ -1558,7 +1569,7 @@ bool place_xcds(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, cons
     slots = std::max(slots, end);
   }
   L->xcd_first[kXcds] = q;
-  if (slots * kXcds > INT32_MAX) return false;
+  if (slots * kXcds > kMaxGrid) return false;
   for (int u = 0; u < U; ++u) L->g[u].xcd_remap = 0;  // pieces index the plain tile order
   L->placed = 1;
   *grid = (int)(slots * kXcds);
@@ -1911,7 +1922,8 @@ void plan_units(const gdy_ctx* ctx, const gdy_gemm* g, gdy_plan_t* p, int mode, 
 void add_bias_sum(BiasSums* s, const float* part, float* out, int n, int rows, int items, int64_t stride);
 hipError_t launch_bias_sums(BiasSums* s, hipStream_t hs, hipEvent_t stop);
 
-// Launch block of members of few rows of one layout: a workgroup a column tile.
+// Launch block of members of few rows of one layout: a workgroup a column tile (max_span
+// at most).
 void build_skinny(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, const Members& members, KLaunch* L,
                   int* grid) {
   L->count = members.size();
@@ -1927,7 +1939,7 @@ void build_skinny(const gdy_ctx* ctx, const gdy_gemm* g, const gdy_plan_t& p, co
       a.tiles_n = (int32_t)((x.n + cols - 1) / cols);
     }
     L->first[u] = (int32_t)wg;
-    wg += (int64_t)a.tiles_m * a.tiles_n * a.batch;
+    wg += std::min((int64_t)a.tiles_m * a.tiles_n * a.batch, max_span(L->count));
   }
   L->first[L->count] = (int32_t)wg;
   *grid = (int)wg;

@@ -341,10 +341,33 @@ def test_batch_strides_past_every_offset(ctx, stride):
         assert run_epilogue(ctx, [single], [zero]) == OK
     far = {"stride_a": 1 << 44, "a": 1 << 46, "batch": 3, "stride_c": 64 * 96, "stride_b": 0}
     assert run_epilogue(ctx, [gemm(**far)], [zero]) == OK
-    most = {"m": 1, "n": 1, "k": 1, "lda": 1, "ldb": 1, "ldc": 1, "batch": (1 << 31) - 2, "stride_a": 1 << 44, "a": 8 << 40}
+    most = {"m": 1, "n": 1, "k": 1, "lda": 1, "ldb": 1, "ldc": 1, "batch": (1 << 31) - (1 << 23), "stride_a": 1 << 44, "a": 8 << 40}
     assert run_epilogue(ctx, [gemm(**dict(most, stride_c=1))], [zero]) == OK
     # (C behind A's start: inside what A's items span)
     assert run_epilogue(ctx, [gemm(**dict(most, stride_c=1, c=9 << 40))], [zero]) == ALIAS
+
+
+def test_members_of_more_work_items_than_workgroups(ctx):
+    """A launch holds fewer than 2^32 threads; members of more work items loop over them, by an index of 31 bits."""
+    ints = [(ctypes.c_int32 * 1)() for _ in range(4)]
+    limit = ((1 << 32) - 1) // 512
+    for op, k in ((gdy.GEMM, 3), (gdy.ADD, 0)):
+        def member(q, batch):
+            return gemm(m=1, n=1, k=k, op=op, lda=3, ldb=1, ldc=1, batch=batch, stride_a=3, stride_b=0, stride_c=1,
+                        a=(4 * q + 1) << 42, b=(4 * q + 2) << 42, c=(4 * q + 3) << 42)
+        for count, batch in ((1, 100), (1, limit - 7), (1, 1 << 26), (2, 1 << 22), (2, 1 << 23), (16, 1 << 20)):
+            g = (gdy.GemmDesc * count)(*[member(q, batch) for q in range(count)])
+            items = (ctypes.c_int64 * count)()
+            assert ctx.lib.gdy_dispatch_map(ctx.h, g, count, gdy.DEFAULT if count == 1 else gdy.GO, count, 0, 1, *ints,
+                                            items) == OK, ctx.last_error()
+            # grid, gemm_of_wg, first_item, item_stride of workgroup 0
+            share = limit // count // 8 * 8
+            assert items[0] == batch and ints[0][0] <= limit and ints[3][0] >= min(batch, share), (op, count, batch)
+            assert ints[1][0] == 0 and ints[2][0] == 0
+        for batch, want in (((1 << 31) - 1 - limit, OK), ((1 << 31) - limit, UNSUPPORTED), ((1 << 31) - 1, UNSUPPORTED)):
+            g = (gdy.GemmDesc * 1)(member(0, batch))
+            assert status(ctx, ctx.lib.gdy_execute, g, 1, gdy.SELECTOR, 0, None, None) == want
+            assert run_epilogue(ctx, list(g), [gdy.EpilogueDesc()]) == want
 
 
 def test_null_arguments(ctx):
