@@ -118,21 +118,22 @@ template <int ACT> __device__ __forceinline__ float act_value(float x) {
   return x;
 }
 
-// f'(x).  Beyond +-64 every slope is 0 or 1 in fp32; the saved value may be
-// infinite where it passed its type's range, and inf * 0 must not enter (NaN does).
+// f'(x).  At and beyond +-128 every slope is 0 or 1 in fp32 (silu's is x exp(x) far below 0, which
+// leaves fp32 at -104; the logistic function's exponential passes its range at -89); the saved
+// value may be infinite where it passed its type's range, and inf * 0 must not enter (NaN does).
 template <int ACT> __device__ __forceinline__ float act_slope(float x) {
   if constexpr (ACT == ACT_RELU) return x <= 0.0f ? 0.0f : 1.0f;
   if constexpr (ACT == ACT_GELU) {
     // Phi(x) + x phi(x) is w = phi's factor exp(-a^2 / 2) times (Q(a) - a / sqrt(2 pi))
     // for x < 0, a = |x|, and 1 - w above
     float a = __builtin_fabsf(x);
-    a = a > 64.0f ? 64.0f : a;
+    a = a > 128.0f ? 128.0f : a;
     float bell;
     const float q = mills(a, bell);
     const float w = bell * __builtin_fmaf(a, -0.3989422804014327f, q);
     return x < 0.0f ? w : 1.0f - w;
   }
-  x = x > 64.0f ? 64.0f : x < -64.0f ? -64.0f : x;
+  x = x > 128.0f ? 128.0f : x < -128.0f ? -128.0f : x;
   if constexpr (ACT == ACT_GELU_TANH) {
     const float x2 = x * x, p = logistic2(x * __builtin_fmaf(-kLog2e * kTanhB, x2, -kLog2e * kTanhA));
     return __builtin_fmaf(x * p * (1.0f - p), __builtin_fmaf(3.0f * kTanhB, x2, kTanhA), p);

@@ -228,3 +228,40 @@ def test_nan_and_infinity_stay_in_their_rows(ctx):
     torch.cuda.synchronize()
     rest = [i for i in range(12) if i != 5]
     assert torch.isfinite(one.c[rest].float()).all() and not torch.isfinite(one.c[5].float()).any()
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_slopes_far_from_zero(ctx, act):
+    """fp32 slopes where they are small, and the limits 0 and 1 at infinity (exactly, whatever they multiply).
+    Down to 2^-119, a slope's exponentials have arguments y of at most 128 in base 2, off by 1.5 * 2^-24 of
+    themselves: a relative error of 1.5 * 2^-24 * 128 ln 2 = 133 * 2^-24 (gelu: the square's rounding too, 178 *
+    2^-24); the reciprocal, the exponential and the products add less than 12 * 2^-24 and its polynomial 2^-20,
+    16 * 2^-24.  The slope of gelu is exp(-x^2/2) (Q - x / sqrt(2 pi)), that of gelu_tanh and silu p (1 + x ...):
+    from 5 on the terms' difference is at least 0.79 of the larger.  Below 5 they are left to other tests."""
+    inf = float("inf")
+    xs = [-inf, -3e38, -1e5, -129.0, -128.0, -120.0, -104.0, -100.0] + \
+        [x for x in (-85.0, -80.0, -75.5, -70.0, -66.0, -64.5, -64.0, -63.0, -50.25, -30.0, -20.0, -12.0, -9.0, -7.5, -6.0, -5.0)] + \
+        [5.0, 20.0, 64.0, 65.0, 100.0, 128.0, 129.0, 1e5, 3e38, inf]
+    z = torch.tensor(xs, device="cuda").repeat(3, 1)
+    dy = torch.tensor([1.0, 2.0 ** 100, -2.0 ** 127], device="cuda")[:, None].expand(3, len(xs)).contiguous()
+    dz = torch.full_like(z, float("nan"))
+    ctx.execute_act_grad(gdy.ActGrad(dy, z, dz, None, act))
+    torch.cuda.synchronize()
+    x = z.double().cpu().clamp(-1000.0, 1000.0)
+    if act == "relu":
+        want = (x > 0).double()
+    elif act == "silu":
+        p = torch.sigmoid(x)
+        want = p * (1 + x * torch.sigmoid(-x))
+    elif act == "gelu":
+        want = torch.special.erfc(-x / 2 ** 0.5) / 2 + x * torch.exp(-x * x / 2) / (2 * torch.pi) ** 0.5
+    else:
+        c = (8 / torch.pi) ** 0.5
+        u = c * (x + 0.044715 * x ** 3)
+        want = torch.sigmoid(u) * (1 + x * torch.sigmoid(-u) * c * (1 + 3 * 0.044715 * x * x))
+    want = want * dy.double().cpu()
+    bound = 2.0 ** -16 * want.abs() + 2.0 ** -119 * dy.double().cpu().abs()
+    close(dz, want, bound, act)
+    ends = z.cpu().abs() >= 128.0
+    exact = torch.where(z.cpu() > 0, dy.cpu(), torch.zeros(()))
+    assert torch.equal(dz.cpu()[ends], exact[ends])
