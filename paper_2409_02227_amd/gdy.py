@@ -236,6 +236,14 @@ class Add:
         return d
 
 
+def _check_device(device, what, *tensors):
+    """An address of another device's memory, or of the host's, faults in a kernel (device
+    < 0, a host-only context: nothing is read)."""
+    for t in tensors:
+        if t is not None and device >= 0 and t.get_device() != device:
+            raise ValueError(f"{what}: a tensor on {t.device}, the context is on cuda:{device}")
+
+
 def _act(act) -> int:
     if isinstance(act, str):
         if act not in ACTS:
@@ -287,6 +295,9 @@ class Epilogue:
     grad: bool = False
     bias_grad: object = None
 
+    def tensors(self):
+        return self.bias, self.residual, self.aux, self.bias_grad
+
     def desc(self, c, items: int = 0) -> EpilogueDesc:
         """For the output tensor c; items: batch items of a 3-D c, or the groups
         that bias and bias_grad may be given for."""
@@ -337,6 +348,9 @@ class Grouped:
     scale_b: float = 1.0
     scales: object = None
     epilogue: object = None
+
+    def tensors(self):
+        return (self.a, self.b, self.c, self.offsets, self.scales) + (self.epilogue.tensors() if self.epilogue else ())
 
     def descs(self):
         """(GroupedDesc, EpilogueDesc or None)."""
@@ -393,6 +407,9 @@ class ActGrad:
     bias_grad: object = None
     act: object = "none"
     offsets: object = None
+
+    def tensors(self):
+        return self.dy, self.z, self.dz, self.bias_grad, self.offsets
 
     def desc(self) -> ActGradDesc:
         d = ActGradDesc()
@@ -509,6 +526,7 @@ class Context:
         if st != 0:
             raise GdyError(st, f"gdy_create failed (see stderr); table={table}")
         self.h = h
+        self.device = device
 
     def close(self):
         if getattr(self, "h", None):
@@ -536,11 +554,21 @@ class Context:
         self._check(self.lib.gdy_plan(self.h, arr, len(gemms), _mode(mode), forced_cd, ctypes.byref(p)))
         return p.as_dict()
 
+    def _epilogue_descs(self, gemms):
+        """epilogue_descs() of members whose tensors all lie on the context's device."""
+        eps = epilogue_descs(gemms)
+        if eps is not None:
+            for g in gemms:
+                e = getattr(g, "epilogue", None)
+                if e is not None:
+                    _check_device(self.device, "a GEMM with an epilogue", g.a, g.b, g.c, *e.tensors())
+        return eps
+
     def execute(self, gemms, mode="selector", forced_cd: int = 0, stream=None, want_plan=False):
         """Launch a submission on `stream` (torch stream, raw handle or None for
         torch's current stream).  Returns the plan dict when want_plan.  Gemm
         objects may carry epilogues."""
-        arr, eps = descs(gemms), epilogue_descs(gemms)
+        arr, eps = descs(gemms), self._epilogue_descs(gemms)
         handle = _stream_handle(stream)
         p = Plan()
         if eps is None:
@@ -554,7 +582,7 @@ class Context:
     def execute_static(self, gemms, mode="selector", forced_cd: int = 0, stream=None, want_plan=False):
         """gdy_execute_static: as execute(), with the split-K planes in the
         library's static device array (no allocation)."""
-        arr, eps = descs(gemms), epilogue_descs(gemms)
+        arr, eps = descs(gemms), self._epilogue_descs(gemms)
         handle = _stream_handle(stream)
         p = Plan()
         if eps is None:
@@ -575,6 +603,7 @@ class Context:
 
     def execute_grouped(self, product: Grouped, stream=None):
         """Launch a product grouped by expert (gdy_execute_grouped)."""
+        _check_device(self.device, "a grouped product", *product.tensors())
         self.execute_grouped_descs(*product.descs(), _stream_handle(stream))
 
     def execute_grouped_descs(self, desc, epilogue, handle):
@@ -584,6 +613,7 @@ class Context:
 
     def execute_act_grad(self, op: ActGrad, stream=None):
         """Launch an activation and bias gradient (gdy_execute_act_grad)."""
+        _check_device(self.device, "an activation gradient", *op.tensors())
         self.execute_act_grad_desc(op.desc(), _stream_handle(stream))
 
     def execute_act_grad_desc(self, desc, handle):

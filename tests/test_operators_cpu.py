@@ -113,6 +113,57 @@ def test_act_grad_shapes():
             bad.desc()
 
 
+def test_tensors_of_another_device(monkeypatch):
+    """Operands that the context's device cannot read (offsets left on the host, above all) never reach the library."""
+    class NoLibrary:
+        def __getattr__(self, name):
+            raise AssertionError(f"{name} reached")
+
+    class Elsewhere:
+        """A tensor's shape and strides on cuda:`at`."""
+        def __init__(self, t, at):
+            self.t, self.at, self.device = t, at, f"cuda:{at}"
+
+        def get_device(self):
+            return self.at
+
+        def __getattr__(self, name):
+            return getattr(self.t, name)
+
+        def __getitem__(self, i):
+            return Elsewhere(self.t[i], self.at)
+
+    ctx = object.__new__(gdy.Context)
+    ctx.h, ctx.lib, ctx.device = None, NoLibrary(), 1
+    def here(*shape, dtype=BF):
+        return Elsewhere(torch.zeros(*shape, dtype=dtype), 1)
+    def operators(change, to):
+        def t(name, *shape, dtype=BF):
+            x = here(*shape, dtype=dtype)
+            return to(x) if name == change else x
+        off = t("offsets", 4, dtype=torch.int32)
+        e = gdy.Epilogue(t("bias", 8), "gelu", t("residual", 10, 8), t("aux", 10, 8), True, t("bias_grad", 8, dtype=torch.float32))
+        yield "gemm", lambda: ctx.execute([gdy.Gemm(t("a", 10, 16), t("b", 16, 8), t("c", 10, 8), epilogue=e)])
+        yield "static", lambda: ctx.execute_static([gdy.Gemm(t("a", 10, 16), t("b", 16, 8), t("c", 10, 8), epilogue=e)])
+        yield "grouped", lambda: ctx.execute_grouped(gdy.Grouped(t("a", 10, 16), t("b", 3, 16, 8), t("c", 10, 8), off, epilogue=e))
+        yield "act_grad", lambda: ctx.execute_act_grad(gdy.ActGrad(t("dy", 10, 8), t("z", 10, 8), t("dz", 10, 8),
+                                                                   t("bias_grad", 8, dtype=torch.float32), "gelu", off))
+    monkeypatch.setattr(gdy, "_stream_handle", lambda *a: None)
+    takes = {"gemm": ("a", "b", "c", "bias", "residual", "aux", "bias_grad"),
+             "grouped": ("a", "b", "c", "bias", "residual", "aux", "bias_grad", "offsets"),
+             "act_grad": ("dy", "z", "dz", "bias_grad", "offsets")}
+    takes["static"] = takes["gemm"]
+    for change in sorted({n for names in takes.values() for n in names}) + [None]:
+        for to in (lambda x: x.t, lambda x: Elsewhere(x.t, 0)):
+            for kind, call in operators(change, to):
+                if change in takes[kind]:
+                    with pytest.raises(ValueError, match="cuda:1"):
+                        call()
+                else:
+                    with pytest.raises(AssertionError, match="reached"):
+                        call()
+
+
 # ---- the library's refusals -------------------------------------------------------
 BASE = 1 << 32  # addresses that nothing reads on a host-only context
 
