@@ -195,6 +195,17 @@ def _dtype_code(t) -> int:
     return _TORCH_DTYPE[t.dtype]
 
 
+def _rows_of(t, name="operands"):
+    """A matrix's leading dimension; its rows must be contiguous and lie apart."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be 2-D (or 3-D batches) with a contiguous last dimension")
+    if t.shape[0] > 1 and t.stride(0) < 1:  # an expanded matrix: no leading dimension reads one row again
+        raise ValueError(f"the rows of {name} must not be one row expanded")
+    if t.shape[0] <= 1:  # a single row's stride says nothing
+        return max(t.stride(0), t.shape[1], 1)
+    return t.stride(0)
+
+
 @dataclass
 class Add:
     """Element-wise C = A + B over an M x N region: the non-GEMM that co-runs
@@ -217,18 +228,16 @@ class Add:
         def mat(t):
             return (t[0], t.stride(0)) if t.dim() == 3 else (t, 0)
         (a2, sa), (b2, sb), (c2, sc) = mat(a), mat(b), mat(c)
-        for t in (a2, b2, c2):
-            if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-                raise ValueError("operands must be 2-D (or 3-D batches) with a contiguous last dimension")
+        lda, ldb, ldc = _rows_of(a2), _rows_of(b2), _rows_of(c2)
         m, n = c2.shape
         if tuple(a2.shape) != (m, n) or tuple(b2.shape) != (m, n):
             raise ValueError("add operands must have C's shape")
         d = GemmDesc()
         d.m, d.n, d.k = m, n, 0
         d.a_type, d.b_type, d.c_type = _dtype_code(a), _dtype_code(b), _dtype_code(c)
-        d.a, d.lda = a.data_ptr(), max(a2.stride(0), 1)
-        d.b, d.ldb = b.data_ptr(), max(b2.stride(0), 1)
-        d.c, d.ldc = c.data_ptr(), max(c2.stride(0), 1)
+        d.a, d.lda = a.data_ptr(), lda
+        d.b, d.ldb = b.data_ptr(), ldb
+        d.c, d.ldc = c.data_ptr(), ldc
         d.scale_a = d.scale_b = 1.0
         d.tenant, d.variant = int(self.tenant), int(self.variant)
         d.batch, d.op = batch, ADD
@@ -252,13 +261,6 @@ def _act(act) -> int:
     return int(act)
 
 
-def _rows_of(t, name):
-    """A matrix's leading dimension; its rows must be contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must have a contiguous last dimension")
-    return max(t.stride(0), 1)
-
-
 def _check_offsets(offsets):
     import torch
     if offsets.dtype != torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.shape[0] < 1:
@@ -274,6 +276,8 @@ def _bias_grad_stride(t, n, items):
     if t.dim() == 1 and tuple(t.shape) == (n,) and (n < 2 or t.stride(0) == 1):
         return 0
     if t.dim() == 2 and tuple(t.shape) == (items, n) and (n < 2 or t.stride(1) == 1):
+        if items > 1 and t.stride(0) == 0:
+            raise ValueError("the rows of bias_grad must not be one row expanded")
         return t.stride(0) if items > 1 else 0
     raise ValueError(f"bias_grad must hold {n} or {items} x {n} values, rows contiguous")
 
@@ -470,9 +474,7 @@ class Gemm:
                 return t[0], t.stride(0)
             return t, 0
         (a2, sa), (b2, sb), (c2, sc) = mat(a), mat(b), mat(c)
-        for t in (a2, b2, c2):
-            if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-                raise ValueError("operands must be 2-D (or 3-D batches) with a contiguous last dimension")
+        lda, ldb, ldc = _rows_of(a2), _rows_of(b2), _rows_of(c2)
         m, n = c2.shape
         k = a2.shape[0] if self.trans_a else a2.shape[1]
         am = a2.shape[1] if self.trans_a else a2.shape[0]
@@ -483,9 +485,9 @@ class Gemm:
         d.m, d.n, d.k = m, n, k
         d.a_type, d.b_type, d.c_type = _dtype_code(a), _dtype_code(b), _dtype_code(c)
         d.trans_a, d.trans_b = int(self.trans_a), int(self.trans_b)
-        d.a, d.lda = a.data_ptr(), max(a2.stride(0), 1)
-        d.b, d.ldb = b.data_ptr(), max(b2.stride(0), 1)
-        d.c, d.ldc = c.data_ptr(), max(c2.stride(0), 1)
+        d.a, d.lda = a.data_ptr(), lda
+        d.b, d.ldb = b.data_ptr(), ldb
+        d.c, d.ldc = c.data_ptr(), ldc
         d.scale_a, d.scale_b = float(self.scale_a), float(self.scale_b)
         d.tenant, d.variant = int(self.tenant), int(self.variant)
         d.batch = batch

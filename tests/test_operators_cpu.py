@@ -113,6 +113,34 @@ def test_act_grad_shapes():
             bad.desc()
 
 
+def test_expanded_and_single_rows():
+    """A matrix expanded from one row has no leading dimension, one column wide least of all (stride 0 was taken as
+    1: rows behind the only one were read).  A single row's stride says nothing."""
+    column, wide = torch.zeros(1, 1, dtype=BF).expand(100, 1), torch.zeros(1, 8, dtype=BF).expand(100, 8)
+    full, one, off = torch.zeros(100, 8, dtype=BF), torch.zeros(100, 1, dtype=BF), torch.zeros(3, dtype=torch.int32)
+    sums = torch.zeros(1, 8).expand(2, 8)
+    w = torch.zeros(2, 1, 8, dtype=BF)
+    bad = [lambda: gdy.ActGrad(column, None, one).desc(), lambda: gdy.ActGrad(one, column, one, act="relu").desc(),
+           lambda: gdy.ActGrad(one, None, column).desc(), lambda: gdy.ActGrad(wide, None, full).desc(),
+           lambda: gdy.ActGrad(full, None, full, sums, offsets=off).desc(),
+           lambda: gdy.Grouped(column, w, full, off).descs(), lambda: gdy.Grouped(one, w, wide, off).descs(),
+           lambda: gdy.Grouped(one, w, full, off, epilogue=gdy.Epilogue(residual=wide)).descs(),
+           lambda: gdy.Grouped(one, w, full, off, epilogue=gdy.Epilogue(bias_grad=sums)).descs(),
+           lambda: gdy.Epilogue(aux=column).desc(one),
+           lambda: gdy.Gemm(column, w[0], full).desc(), lambda: gdy.Gemm(one, w[0], wide).desc(),
+           lambda: gdy.Gemm(torch.zeros(8, 100, dtype=BF), column, torch.zeros(8, 1, dtype=BF)).desc(),
+           lambda: gdy.Add(one, one, column).desc(), lambda: gdy.Add(column, one, one).desc()]
+    for x in bad:
+        with pytest.raises(ValueError, match="expanded"):
+            x()
+    row = torch.zeros(16, 1, dtype=BF).t()  # 1 x 16, strides (1, 1)
+    d = gdy.Gemm(row, torch.zeros(16, 8, dtype=BF), torch.zeros(8, 1, dtype=BF).t()).desc()
+    assert (d.lda, d.ldb, d.ldc) == (16, 8, 8)
+    assert gdy.Gemm(torch.zeros(4, 32, dtype=BF)[:1, :16], torch.zeros(16, 8, dtype=BF), torch.zeros(1, 8, dtype=BF)).desc().lda == 32
+    assert gdy.Add(row, row, row).desc().ldc == 16 and gdy.ActGrad(row, None, row).desc().lddy == 16
+    assert gdy.Gemm(one.t(), one, torch.zeros(1, 1, dtype=BF)).desc().k == 100
+
+
 def test_tensors_of_another_device(monkeypatch):
     """Operands that the context's device cannot read (offsets left on the host, above all) never reach the library."""
     class NoLibrary:
