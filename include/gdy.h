@@ -419,6 +419,13 @@ gdy_status gdy_execute_grouped(gdy_ctx* ctx, const gdy_grouped* product, const g
                                void* hip_stream);
 
 /*
+ * The tile of C, rows x cols, that a workgroup of gdy_execute_grouped computes for this
+ * product (its last tiles of 256 rows may run as halves); 0 x 0 where no workgroup
+ * runs.  Checks the product as the call does; host only, also on host-only contexts.
+ */
+gdy_status gdy_grouped_tile(gdy_ctx* ctx, const gdy_grouped* product, int32_t* rows, int32_t* cols);
+
+/*
  * Activation and bias gradients that no product precedes:
  *   dz(i,j) = round(dy(i,j) * f'(z(i,j)));  bias_grad_e(j) = the sum of dy * f'(z) over the rows of e,
  * before its rounding, in fp32 and in an order that the sizes and offsets fix.  All

@@ -2734,6 +2734,24 @@ gdy_status gdy_execute_grouped(gdy_ctx* ctx, const gdy_grouped* product, const g
   }
 }
 
+gdy_status gdy_grouped_tile(gdy_ctx* ctx, const gdy_grouped* product, int32_t* rows, int32_t* cols) {
+  if (!ctx) return GDY_ERR_INVALID_ARG;
+  ctx->err.clear();
+  try {
+    if (!product || !rows || !cols) return fail(ctx, GDY_ERR_INVALID_ARG, "null product, rows or cols");
+    const gdy_status s = validate_grouped(ctx, *product, nullptr);
+    if (s != GDY_OK) return s;
+    *rows = *cols = 0;
+    if (!group_has_tiles(*product)) return GDY_OK;
+    const GroupChoice c = choose_group_kernel(ctx, *product);
+    *rows = c.bm;
+    *cols = c.kern.bn;
+    return GDY_OK;
+  } catch (...) {
+    return fail(ctx, GDY_ERR_NOMEM, "host allocation failed");
+  }
+}
+
 gdy_status gdy_execute_act_grad(gdy_ctx* ctx, const gdy_act_grad* op, void* hip_stream) {
   if (!ctx) return GDY_ERR_INVALID_ARG;
   ctx->err.clear();

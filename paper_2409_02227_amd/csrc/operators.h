@@ -349,14 +349,47 @@ int group_k_tile(const gdy_ctx* ctx, const gdy_grouped& g, bool copies) {
   return tiles(128) > ctx->cus ? 1 : 2;
 }
 
+// Whether both operands of a product take copies, its kernel and the rows of a tile.
+struct GroupChoice {
+  bool a_copies, b_copies;
+  GroupKernel kern;
+  int bm;
+};
+GroupChoice choose_group_kernel(const gdy_ctx* ctx, const gdy_grouped& g) {
+  const bool over_k = g.over == GDY_OVER_K;
+  const int es = elem_size(g.a_type);
+  GroupChoice c;
+  c.a_copies = copies_ok(g.a, g.lda, g.k, es, !over_k, 0);
+  c.b_copies = copies_ok(g.b, g.ldb, g.k, es, !over_k && g.trans_b, over_k || g.groups == 1 ? 0 : g.stride_b);
+  const bool copies = c.a_copies && c.b_copies;
+  if (over_k) {
+    c.kern = group_kernel_of(g.a_type, 1, 0, group_k_tile(ctx, g, copies));
+    c.bm = c.kern.bm;
+  } else if (group_rows_few(g, copies)) {
+    c.kern = group_few(g.a_type, g.trans_b);
+    c.bm = c.kern.bm;
+  } else {
+    const GroupTileCost& tile = group_rows_tile(ctx, g, copies);
+    c.kern = group_kernel_of(g.a_type, 0, g.trans_b, tile.tile);
+    c.bm = tile.bm;
+  }
+  return c;
+}
+
+// Whether a valid product computes a tile at all.
+bool group_has_tiles(const gdy_grouped& g) {
+  return g.groups > 0 && g.n > 0 && (g.over == GDY_OVER_K ? g.k : g.rows) > 0;
+}
+
 gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue* ep, hipStream_t hs) {
   const bool over_k = g.over == GDY_OVER_K;
   const int es = elem_size(g.a_type), os = g.c_type == GDY_F32 ? 4 : 2;
   const int64_t m = over_k ? g.k : g.rows;
   float* bias_grad = ep ? ep->bias_grad : nullptr;
   const bool shared = g.groups > 1 && ep && ep->stride_bias_grad == 0;
-  if (g.groups == 0 || g.n == 0 || (m == 0 && !bias_grad)) return GDY_OK;
-  if (m == 0) {  // no rows: zero sums
+  if (!group_has_tiles(g)) {
+    if (g.groups == 0 || g.n == 0 || !bias_grad) return GDY_OK;
+    // no rows: zero sums
     BiasSums s;
     s.count = 0;
     add_bias_sum(&s, nullptr, bias_grad, (int)g.n, 0, shared ? 1 : g.groups, ep->stride_bias_grad);
@@ -381,19 +414,15 @@ gdy_status launch_grouped(gdy_ctx* ctx, const gdy_grouped& g, const gdy_epilogue
   a.ldb = (int32_t)g.ldb;
   a.ldc = (int32_t)g.ldc;
   a.scale = g.scale_a * g.scale_b;
-  a.a_dma = copies_ok(g.a, g.lda, g.k, es, !over_k, 0);
-  a.b_dma = copies_ok(g.b, g.ldb, g.k, es, !over_k && g.trans_b, over_k || g.groups == 1 ? 0 : g.stride_b);
   auto vec = [&](const void* p, int64_t ld, int64_t stride) {
     return (uintptr_t)p % 8 == 0 && (ld * os) % 8 == 0 && (!over_k || g.groups == 1 || (stride * os) % 8 == 0);
   };
   a.c_vec = vec(g.c, g.ldc, g.stride_c);
-  const bool copies = a.a_dma && a.b_dma;
-  const GroupTileCost* rows_tile = over_k ? nullptr : &group_rows_tile(ctx, g, copies);
-  const bool few = !over_k && group_rows_few(g, copies);
-  const GroupKernel kern =
-      few ? group_few(g.a_type, g.trans_b)
-          : group_kernel_of(g.a_type, over_k, g.trans_b, over_k ? group_k_tile(ctx, g, copies) : rows_tile->tile);
-  a.bm = over_k || few ? kern.bm : rows_tile->bm;
+  const GroupChoice choice = choose_group_kernel(ctx, g);
+  const GroupKernel& kern = choice.kern;
+  a.a_dma = choice.a_copies;
+  a.b_dma = choice.b_copies;
+  a.bm = choice.bm;
   a.max_slots = (int32_t)max_row_tiles(g.rows, g.groups, a.bm);
   a.xcd_cus = std::max(ctx->cus / kXcds, 1);
   const int sums_per_tile = !over_k && a.bm == 256 ? 2 : 1;

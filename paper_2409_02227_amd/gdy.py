@@ -40,7 +40,8 @@ STATUS = {0: "GDY_OK", 1: "GDY_ERR_INVALID_ARG", 2: "GDY_ERR_UNSUPPORTED", 3: "G
           4: "GDY_ERR_TOO_MANY", 5: "GDY_ERR_TABLE", 6: "GDY_ERR_HIP", 7: "GDY_ERR_NOMEM"}
 
 EXPORTS = ("gdy_create", "gdy_destroy", "gdy_set_rc", "gdy_plan", "gdy_execute", "gdy_execute_static",
-           "gdy_execute_epilogue", "gdy_execute_epilogue_static", "gdy_execute_grouped", "gdy_execute_act_grad",
+           "gdy_execute_epilogue", "gdy_execute_epilogue_static", "gdy_execute_grouped", "gdy_grouped_tile",
+           "gdy_execute_act_grad",
            "gdy_set_timing", "gdy_last_kernel_times", "gdy_kernel_times", "gdy_features", "gdy_dispatch_map",
            "gdy_variant_count",
            "gdy_variant_info", "gdy_variant_find", "gdy_isolated_variant",
@@ -156,6 +157,7 @@ def load_library(path: str = None) -> ctypes.CDLL:
         "gdy_execute_epilogue_static": (i32, [P, ctypes.POINTER(GemmDesc), ctypes.POINTER(EpilogueDesc), i32, i32,
                                               i32, P, ctypes.POINTER(Plan)]),
         "gdy_execute_grouped": (i32, [P, ctypes.POINTER(GroupedDesc), ctypes.POINTER(EpilogueDesc), P]),
+        "gdy_grouped_tile": (i32, [P, ctypes.POINTER(GroupedDesc), ctypes.POINTER(i32), ctypes.POINTER(i32)]),
         "gdy_execute_act_grad": (i32, [P, ctypes.POINTER(ActGradDesc), P]),
         "gdy_set_timing": (i32, [P, i32]),
         "gdy_last_kernel_times": (i32, [P, ctypes.POINTER(ctypes.c_float),
@@ -612,6 +614,13 @@ class Context:
         """Launch a prepared GroupedDesc (epilogue: an EpilogueDesc or None)."""
         self._check(self.lib.gdy_execute_grouped(self.h, ctypes.byref(desc),
                                                  None if epilogue is None else ctypes.byref(epilogue), handle))
+
+    def grouped_tile(self, product):
+        """(rows, columns) of the tile that a Grouped or GroupedDesc runs on (gdy_grouped_tile)."""
+        d = product if isinstance(product, GroupedDesc) else product.descs()[0]
+        rows, cols = ctypes.c_int32(), ctypes.c_int32()
+        self._check(self.lib.gdy_grouped_tile(self.h, ctypes.byref(d), ctypes.byref(rows), ctypes.byref(cols)))
+        return rows.value, cols.value
 
     def execute_act_grad(self, op: ActGrad, stream=None):
         """Launch an activation and bias gradient (gdy_execute_act_grad)."""
