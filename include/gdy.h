@@ -360,6 +360,7 @@ typedef struct {
  * Every pointer is aligned to its elements.  The split-K workspace also holds the
  * partial column sums of a group's bias gradients: a group that needs more of both
  * than the workspace has is refused (GDY_ERR_UNSUPPORTED) before anything launches.
+ * Replays of graphs captured from one context share its workspace too, and must be ordered.
  */
 gdy_status gdy_execute_epilogue(gdy_ctx* ctx, const gdy_gemm* gemms, const gdy_epilogue* epilogues, int32_t n,
                                 int32_t mode, int32_t forced_cd, void* hip_stream, gdy_plan_t* out);
@@ -410,7 +411,8 @@ typedef struct {
  * groups x n (stride_bias 0: shared); stride_r and stride_aux are ignored.  Over K
  * it may hold a residual only (R_e at stride_r; C itself accumulates into it).
  * Aliasing rules as for gdy_execute_epilogue.  Allocates nothing; bias gradients use the
- * context's split-K workspace (calls of one context must be ordered) and are refused
+ * context's split-K workspace (calls of one context, and replays of graphs captured from
+ * them, must be ordered) and are refused
  * (GDY_ERR_UNSUPPORTED) where a fp32 row of n for each tile of 16 to 256 rows does
  * not fit into it.  Over K, A and B must end within 2 GiB; over rows only a group's B,
  * and 512 rows of A and of C, have to.
@@ -431,7 +433,12 @@ gdy_status gdy_grouped_tile(gdy_ctx* ctx, const gdy_grouped* product, int32_t* r
  * before its rounding, in fp32 and in an order that the sizes and offsets fix.  All
  * matrices are rows x n of `type` (F16, BF16 or F32).  offsets as for gdy_grouped (rows
  * of no group are left as they were), or NULL: one group of all rows.  dz may be
- * dy or z itself (same pointer and leading dimension).
+ * dy or z itself (same pointer and leading dimension).  Asynchronous on `hip_stream`;
+ * allocates nothing.  Bias gradients of more than 32 rows, or of groups, use the context's
+ * split-K workspace, as gdy_execute_grouped's do (calls of one context, and replays of
+ * graphs captured from them, must be ordered), and are refused (GDY_ERR_UNSUPPORTED) where
+ * a fp32 row of n for each 32 rows of a group does not fit into it.  512 rows of each matrix
+ * must end within 2 GiB.
  */
 typedef struct {
   int64_t rows, n;

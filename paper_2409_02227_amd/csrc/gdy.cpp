@@ -1615,7 +1615,7 @@ const void* lone_epilogue_kernel(int dtype, int family, int code, bool copies) {
 }
 
 // Whether a GEMM with an epilogue runs on the kernel of few rows (skinny.h: K in at
-// most two rounds of its loads), alone and beside others, whatever kernel the plan
+// most two of its rounds), alone and beside others, whatever kernel the plan
 // names.
 bool skinny(const gdy_gemm& g, const gdy_epilogue& e) {
   const int es = elem_size(g.a_type);

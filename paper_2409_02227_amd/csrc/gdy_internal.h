@@ -243,7 +243,7 @@ const void* ep_lone_f16(int family, int code, bool copies);
 const void* ep_lone_fp8(int family, int code, bool copies);
 const void* ep_lone_f32(int family, int code, bool copies);
 // GEMMs of at most kSkinnyRows rows, by type and transposed B (null: none); the columns
-// of a workgroup, and the K bytes that its eight waves have in flight at a time.
+// of a workgroup, the K bytes of a wave's step, and the steps of a round.
 constexpr int kSkinnyRows = 16;
 const void* skinny_ep(int dt, int tb);
 constexpr int skinny_cols(int tb) { return tb ? 16 : 64; }

@@ -305,8 +305,11 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
     };
 
     // Tiles that the register way of a kernel with epilogues holds in registers: HBM
-    // answers after 1.7 us, several times what a tile's arithmetic takes, so a tile is
-    // loaded that many before it is computed.  128 x 128 tiles have no registers left.
+    // answers after 1.7 us, several times what a tile's arithmetic takes, so a tile's loads
+    // are issued that many tiles before it is computed.  They are conditional (none past the
+    // last tile), so the compiler's waits assume that none followed: each tile waits for the
+    // loads issued one tile before as well, and the depth is one in effect (about 1 us a K tile of
+    // (509, 2047, 1021) fp16).  128 x 128 tiles have no registers left.
     constexpr int HELD = !EP::on || BM * BN > 64 * 128 ? 0 : BM * BN > 64 * 64 || BN > 64 ? 2 : 3;
     if (ANY && HELD > 0 && nk > 0 && !(acopy && bcopy)) {
       if constexpr (ANY && HELD > 0) {

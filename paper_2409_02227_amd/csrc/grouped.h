@@ -143,7 +143,10 @@ __device__ __forceinline__ KArgs tile_args(const KGroup& g, const uint8_t* a, co
   return p;
 }
 
-// Tile families: the 256 x 256 kernel, and tiles of go_kernel_u.h.
+// Tile families: the 256 x 256 kernel, and tiles of go_kernel_u.h.  The latter run the loop
+// for any operands, also where both take copies: a K step's fragments are read in front of
+// its MFMAs, not a K tile's ahead of them (u_tiles; plain 128 x 128 launches gain 10% by that), and
+// the cost model of their tiles is fitted to that loop.
 template <int DT, int TA, int TB> struct TileP {
   static constexpr int BM = 256, BN = 256, NT = 512, LDS = kPLds;
   static __device__ __forceinline__ void run(const KArgs& p, lds_u8* smem, const GroupEpi& e) {

@@ -313,9 +313,9 @@ const GroupTileCost& group_rows_tile(const gdy_ctx* ctx, const gdy_grouped& g, b
 
 // Whether a product over rows runs in tiles of 16 rows with K over a workgroup's waves
 // (skinny.h).  Few workgroups wait for one K tile after another (32 x 64 tiles: 0.22 to 0.42 us
-// each); these wait for a round of loads, 2 to 4 KiB of a row, in 2.5 us (K x N of 16-bit
-// types, whose loads are 8 bytes, 3.6, and 1.3 TB/s of weights in place of 4), but
-// read a group's B once for 16 rows, from L2 at 8 TB/s.  us, 32 x 64 tiles and these: bf16 nt
+// each); these take a round of loads, 2 to 4 KiB of a row, in 2.5 us as the compiler has it,
+// several waits for memory (skinny.h; K x N of 16-bit types, which waits for all loads two or
+// three times a step, 3.6, and 1.3 TB/s of weights in place of 4), but read a group's B once for 16 rows, from L2 at 8 TB/s.  us, 32 x 64 tiles and these: bf16 nt
 // 65 rows, 768 x 4096 20.7 and 11.0; 2 rows of 128 groups, 4096 x 4096 21.2 and 10.3; 64
 // rows, 4096 x 4096 20.7 and 32.2; nn 2 rows of 16 groups, 72 x 4096 20.8 and 12.2, a row,
 // 4096 x 14336 62.4 and 88.5; fp32 nn 65 rows, 768 x 4096 58.8 and 29.3; fp8 nt 64 rows in

@@ -5,11 +5,17 @@
 // A workgroup of eight waves owns 16 columns (B stored N x K) or 64 (K x N), the
 // waves an eighth of K each.  Both operands go from global memory straight into MFMA
 // fragments: nothing is shared between waves, so there is no LDS stage, no barrier
-// and no tile loop to fill, and a wave keeps 16 (32) KiB of B in flight.  The waves'
-// sums meet in LDS, are added in wave order and leave through the epilogue, so a
-// K needs no second kernel: (1, 2048, 2048) bf16 11.6 us on the tile kernels (two runs and
-// their reduction), 7.2 here.  A wave has a fixed number of steps in flight and waits
-// for HBM between them, so this holds while K takes it at most two rounds (M = 1 and 16, N =
+// and no tile loop to fill.  The waves' sums meet in LDS, are added in wave order and
+// leave through the epilogue, so a K needs no second kernel: (1, 2048, 2048) bf16 11.6 us on
+// the tile kernels (two runs and their reduction), 7.2 here; K x N 9.0.
+//
+// A wave takes K in rounds of AHEAD steps: loads of 8 KiB of B (K x N: 16), then their
+// MFMAs.  The source orders no more than that, and the compiler moves loads behind MFMAs: of
+// a round's 16 loads of N x K, 16- and 8-bit types have 9 to 12 under way before the first
+// wait, fp32 4; of K x N's 20 or 36, 4 to 10, and some waits are for all of them.  A round is so a
+// chain of two to ten trips to HBM and not one, and what bounds this kernel where K is long.
+// The times here and the rules that choose this kernel are of the code as it is.  It holds
+// while K takes a wave at most two rounds (M = 1 and 16, N =
 // 256 to 8192, weights from HBM, tile kernels against this one: bf16 N x K, K = 2048, one
 // round, 14-16 and 9-15 us; K = 8192, four, 14-37 and 14-42; K x N, K = 2048, two, 14-17 and 9-14;
 // K = 8192, eight, 16-38 and 26-47; fp8 N x K, K = 8192, two, 14-25 and 9-22).
@@ -37,7 +43,7 @@ template <int DT, int TB> struct Skinny {
   static constexpr int KB = skinny_kstep(ES);     // K bytes of a step
   static constexpr int AV = KB / 64;              // 16-byte loads of a lane's K bytes
   static constexpr int KROWS = 16 / ES;           // K x N: rows of a lane's K bytes
-  static constexpr int AHEAD = skinny_ahead(ES, TB);  // steps in flight
+  static constexpr int AHEAD = skinny_ahead(ES, TB);  // steps of a round
   static constexpr int PITCH = BN * 4 + 16;
   static constexpr int TABLE = NW * BM * PITCH;   // column sums behind the waves' blocks
   static constexpr int LDS = TABLE + BM * BN * 4;
