@@ -558,6 +558,9 @@ class Context:
         self._check(self.lib.gdy_plan(self.h, arr, len(gemms), _mode(mode), forced_cd, ctypes.byref(p)))
         return p.as_dict()
 
+    def _stream_device(self):
+        return self.device if self.device >= 0 else None
+
     def _epilogue_descs(self, gemms):
         """epilogue_descs() of members whose tensors all lie on the context's device."""
         eps = epilogue_descs(gemms)
@@ -570,10 +573,10 @@ class Context:
 
     def execute(self, gemms, mode="selector", forced_cd: int = 0, stream=None, want_plan=False):
         """Launch a submission on `stream` (torch stream, raw handle or None for
-        torch's current stream).  Returns the plan dict when want_plan.  Gemm
+        torch's current stream of the context's device).  Returns the plan dict when want_plan.  Gemm
         objects may carry epilogues."""
         arr, eps = descs(gemms), self._epilogue_descs(gemms)
-        handle = _stream_handle(stream)
+        handle = _stream_handle(stream, self._stream_device())
         p = Plan()
         if eps is None:
             self._check(self.lib.gdy_execute(self.h, arr, len(gemms), _mode(mode), forced_cd,
@@ -587,7 +590,7 @@ class Context:
         """gdy_execute_static: as execute(), with the split-K planes in the
         library's static device array (no allocation)."""
         arr, eps = descs(gemms), self._epilogue_descs(gemms)
-        handle = _stream_handle(stream)
+        handle = _stream_handle(stream, self._stream_device())
         p = Plan()
         if eps is None:
             self._check(self.lib.gdy_execute_static(self.h, arr, len(gemms), _mode(mode), forced_cd,
@@ -608,7 +611,7 @@ class Context:
     def execute_grouped(self, product: Grouped, stream=None):
         """Launch a product grouped by expert (gdy_execute_grouped)."""
         _check_device(self.device, "a grouped product", *product.tensors())
-        self.execute_grouped_descs(*product.descs(), _stream_handle(stream))
+        self.execute_grouped_descs(*product.descs(), _stream_handle(stream, self._stream_device()))
 
     def execute_grouped_descs(self, desc, epilogue, handle):
         """Launch a prepared GroupedDesc (epilogue: an EpilogueDesc or None)."""
@@ -625,7 +628,7 @@ class Context:
     def execute_act_grad(self, op: ActGrad, stream=None):
         """Launch an activation and bias gradient (gdy_execute_act_grad)."""
         _check_device(self.device, "an activation gradient", *op.tensors())
-        self.execute_act_grad_desc(op.desc(), _stream_handle(stream))
+        self.execute_act_grad_desc(op.desc(), _stream_handle(stream, self._stream_device()))
 
     def execute_act_grad_desc(self, desc, handle):
         """Launch a prepared ActGradDesc."""
@@ -698,10 +701,11 @@ def _mode(mode) -> int:
     return MODES[mode] if isinstance(mode, str) else int(mode)
 
 
-def _stream_handle(stream):
+def _stream_handle(stream, device=None):
+    """None: torch's current stream of `device`, or of the current device."""
     if stream is None:
         import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
     if hasattr(stream, "cuda_stream"):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))

@@ -192,6 +192,33 @@ def test_tensors_of_another_device(monkeypatch):
                         call()
 
 
+def test_the_current_stream_is_the_contexts_devices(monkeypatch):
+    """Without a stream a call runs on the current stream of the context's device, whichever device is current."""
+    import types
+    seen = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: seen.append((name, [a.value for a in args if isinstance(a, ctypes.c_void_p)])) or 0
+
+    monkeypatch.setattr(torch.cuda, "current_stream",
+                        lambda device=None: types.SimpleNamespace(cuda_stream=100 + (0 if device is None else device)))
+    monkeypatch.setattr(gdy, "_check_device", lambda *a: None)
+    ctx = object.__new__(gdy.Context)
+    ctx.h, ctx.lib, ctx.device = None, Library(), 3
+    a, b, c, off = torch.zeros(10, 16, dtype=BF), torch.zeros(16, 8, dtype=BF), torch.zeros(10, 8, dtype=BF), torch.zeros(2, dtype=torch.int32)
+    for g in (gdy.Gemm(a, b, c), gdy.Gemm(a, b, c, epilogue=gdy.Epilogue(act="relu"))):
+        ctx.execute([g])
+        ctx.execute_static([g])
+    ctx.execute_grouped(gdy.Grouped(a, b[None], c, off))
+    ctx.execute_act_grad(gdy.ActGrad(c, c, c, act="relu"))
+    ctx.execute([gdy.Gemm(a, b, c)], stream=7)
+    names = [n for n, _ in seen]
+    assert names == ["gdy_execute", "gdy_execute_static", "gdy_execute_epilogue", "gdy_execute_epilogue_static",
+                     "gdy_execute_grouped", "gdy_execute_act_grad", "gdy_execute"]
+    assert [v[-1] for _, v in seen] == [103] * 6 + [7], seen
+
+
 # ---- the library's refusals -------------------------------------------------------
 BASE = 1 << 32  # addresses that nothing reads on a host-only context
 
