@@ -283,8 +283,8 @@ def prepare_own(s):
     if c["op"] == "route":
         s["desc"] = gdy.Route(x["ids"], s["slots"], s["offsets"]).desc()
     elif c["op"] == "dispatch":
-        s["desc"] = gdy.Dispatch(x["x"], x["slots"], s["out"], weights=x.get("weights"), z=x.get("z"),
-                                 weight_grad=s["dw"]).desc()
+        s["desc"] = gdy.Scatter(x["x"], x["slots"], s["out"], weights=x.get("weights"), z=x.get("z"),
+                                weight_grad=s["dw"]).desc()
     elif c["op"] == "combine":
         s["desc"] = gdy.Combine(x["z"], x["slots"], s["y"], weights=x.get("weights"),
                                 residual=x.get("residual")).desc()
@@ -316,7 +316,7 @@ def run(s):
     elif op == "route":
         s["ctx"].execute_route_desc(s["desc"], s["stream"])
     elif op == "dispatch":
-        s["ctx"].execute_dispatch_desc(s["desc"], s["stream"])
+        s["ctx"].execute_scatter_desc(s["desc"], s["stream"])
     elif op == "combine":
         s["ctx"].execute_combine_desc(s["desc"], s["stream"])
     else:
