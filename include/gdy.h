@@ -456,6 +456,131 @@ typedef struct {
 gdy_status gdy_execute_act_grad(gdy_ctx* ctx, const gdy_act_grad* op, void* hip_stream);
 
 /*
+ * Tokens and experts: what a mixture of experts does around its grouped products.  Token t
+ * sends a row to each of its top_k experts; slots (device, tokens x top_k, contiguous) names
+ * the row of every pair (t, j) among the rows sorted by expert, -1: none.  No two pairs of a
+ * call may have the same row; slots outside 0 .. rows - 1 are none.  Rows that no slot names
+ * are left as they were.  All calls are asynchronous on `hip_stream` and allocate nothing;
+ * outputs may overlap nothing else but where it is said.  Leading dimensions are at most
+ * 2^44, matrices of any alignment of their elements.
+ *
+ * Routing: ids[t * ld_ids + j] is the expert of pair (t, j); ids outside 0 .. experts - 1 are none
+ * (the share of another GPU, padding).  The pairs sorted by expert, those of one expert in
+ * the order of t * top_k + j, are the rows:
+ *   offsets[e] = the number of pairs of the experts below e (experts + 1 values: the
+ *                bounds of gdy_execute_grouped)
+ *   slots[t * top_k + j] = the row of the pair, -1 where it has none
+ * All of both are written.  More than GDY_ROUTE_ALONE pairs use the context's split-K workspace
+ * (calls of one context, and replays of graphs captured from them, must be ordered).
+ */
+#define GDY_MAX_TOP_K 64
+#define GDY_ROUTE_ALONE 4096
+typedef struct {
+  int64_t tokens;                   /* tokens x top_k at most 2^24                          */
+  int32_t top_k;                    /* 1 .. GDY_MAX_TOP_K                                   */
+  int32_t experts;                  /* 0 .. GDY_MAX_GROUPS                                  */
+  const void* ids; int64_t ld_ids;  /* device, tokens x top_k                               */
+  int32_t id_bytes;                 /* 4 or 8: int32_t or int64_t                           */
+  int32_t reserved;                 /* must be 0                                            */
+  int32_t* slots;                   /* device, tokens x top_k                               */
+  int32_t* offsets;                 /* device, experts + 1                                  */
+} gdy_route;
+gdy_status gdy_execute_route(gdy_ctx* ctx, const gdy_route* op, void* hip_stream);
+
+/*
+ * Rows to the experts, and the gradient of the weighted sum that brings them back:
+ *   out[slots(t,j)][:] = round(w(t,j) * x[t][:])           (without weights: x[t][:] itself)
+ *   weight_grad(t,j) = sum_c x[t][c] * z[slots(t,j)][c]     (0 where the pair has no row)
+ * With x the gradient of gdy_execute_combine's y, out is the gradient of its z and
+ * weight_grad that of its weights.  The gradient of out with respect to x is
+ * gdy_execute_combine without weights.
+ */
+typedef struct {
+  int64_t tokens, rows, n;          /* x: tokens x n; out, z: rows x n                      */
+  int32_t top_k;                    /* 1 .. GDY_MAX_TOP_K                                   */
+  int32_t type;                     /* F16, BF16, F32; without weights FP8_E4M3 too         */
+  const int32_t* slots;
+  const void* x; int64_t ldx;
+  const void* weights;              /* device, tokens x top_k, contiguous, or NULL: 1       */
+  int32_t weights_type;             /* GDY_F32 or `type` (ignored without weights)          */
+  int32_t reserved;                 /* must be 0                                            */
+  void* out; int64_t ldo;
+  const void* z; int64_t ldz;       /* read for weight_grad                                 */
+  float* weight_grad;               /* device, tokens x top_k, or NULL; needs weights and z */
+} gdy_scatter;
+gdy_status gdy_execute_scatter(gdy_ctx* ctx, const gdy_scatter* op, void* hip_stream);
+
+/*
+ * Rows back from the experts: y[t][:] = round(sum_j w(t,j) * z[slots(t,j)][:] + R[t][:]), in fp32
+ * in the order of j.  y may be R itself (same pointer and leading dimension).
+ */
+typedef struct {
+  int64_t tokens, rows, n;          /* y, R: tokens x n; z: rows x n                        */
+  int32_t top_k;                    /* 1 .. GDY_MAX_TOP_K                                   */
+  int32_t type;                     /* F16, BF16 or F32                                     */
+  const int32_t* slots;
+  const void* z; int64_t ldz;
+  const void* weights;              /* device, tokens x top_k, contiguous, or NULL: 1       */
+  int32_t weights_type;             /* GDY_F32 or `type` (ignored without weights)          */
+  int32_t reserved;                 /* must be 0                                            */
+  const void* residual; int64_t ldr;  /* R, or NULL                                         */
+  void* y; int64_t ldy;
+} gdy_combine;
+gdy_status gdy_execute_combine(gdy_ctx* ctx, const gdy_combine* op, void* hip_stream);
+
+/*
+ * Rows in 8-bit integers, a scale for each:
+ *   scale_i = max_c |x[i][c]| / 127,  q[i][c] = 127 * x[i][c] / max_c |x[i][c]| rounded to
+ * the nearest integer (the exact quotient, halves to even), so that scale_i * q[i][c] stands for
+ * x[i][c].  A row of zeros has scale 0; a row that holds an infinity or a NaN has one of
+ * them as its scale and codes of 0, so that its products are NaN.  With slots, row i of x goes
+ * to the rows slots(i, 0 .. top_k - 1) of q and scales (as gdy_execute_scatter's); without, to row i.
+ */
+typedef struct {
+  int64_t rows, n;                  /* of x                                                 */
+  int32_t type;                     /* of x: F16, BF16 or F32                               */
+  int32_t top_k;                    /* with slots: 1 .. GDY_MAX_TOP_K; otherwise 0          */
+  const void* x; int64_t ldx;
+  const int32_t* slots;             /* device, rows x top_k, or NULL                        */
+  int64_t out_rows;                 /* with slots: rows of q and scales; otherwise 0        */
+  int8_t* q; int64_t ldq;
+  float* scales;                    /* device, a value a row of q                           */
+} gdy_quantize;
+gdy_status gdy_execute_quantize(gdy_ctx* ctx, const gdy_quantize* op, void* hip_stream);
+
+/*
+ * Products of 8-bit integers with a scale for each row of A (token) and each column of C
+ * (channel):
+ *   z(i,j) = row_scales[i] * col_scales[j] * sum_k A[i][k] op(B)(k,j) + bias(j)
+ *   C(i,j) = round(f(z) + R(i,j))
+ * The sums are exact (32-bit integers; k is at most 131071); each of the products with the
+ * scales, and the rest, is fp32.  With offsets, a product grouped by expert over rows, as
+ * gdy_execute_grouped: the rows offsets[e] .. offsets[e+1] - 1 of A and C belong to group e, with
+ * its own B, column scales and bias; offsets are clamped to 0 .. rows, rows of no group left as
+ * they were.  Without, one product of all rows (groups and the strides are ignored).  The epilogue
+ * may hold a bias, an activation and a residual (R may be C itself; stride_bias counts
+ * between groups).  Allocates nothing and uses no workspace.  A group's B, and 512 rows of A and
+ * of C, must end within 2 GiB.  Non-finite scales give what the formulas give.
+ */
+typedef struct {
+  int64_t rows, n, k;               /* A rows x k, B k x n (trans_b: n x k), C rows x n     */
+  int32_t c_type;                   /* F16, BF16 or F32                                     */
+  int32_t trans_b;                  /* 0 or 1                                               */
+  int32_t groups;                   /* with offsets: 0 .. GDY_MAX_GROUPS                    */
+  int32_t reserved;                 /* must be 0                                            */
+  const int32_t* offsets;           /* device, or NULL                                      */
+  const int8_t* a; int64_t lda;
+  const int8_t* b; int64_t ldb;
+  int64_t stride_b;                 /* between groups of B                                  */
+  const float* row_scales;          /* device, rows values, or NULL: 1                      */
+  const float* col_scales;          /* device, n values a group, or NULL: 1                 */
+  int64_t stride_col_scales;        /* between groups; 0: shared                            */
+  void* c; int64_t ldc;
+} gdy_integer;
+gdy_status gdy_execute_integer(gdy_ctx* ctx, const gdy_integer* product, const gdy_epilogue* epilogue,
+                               void* hip_stream);
+
+/*
  * Per-kernel timing (Sec. 5.3 measures each GEMM's kernel runtime, with the
  * GEMMs run back-to-back on their streams).  When enabled, every dispatch
  * of gdy_execute records a start and a stop event on the stream it runs on

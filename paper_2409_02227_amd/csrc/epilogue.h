@@ -27,6 +27,7 @@ struct EpiOut {
   int c_bytes, ldc, m, n;  // m, n: rows and columns of the matrix
   bool c_vec;
   float scale;
+  const float *row_scales, *col_scales;  // products of 8-bit integers (null: 1), not set for others
   const uint8_t *bias, *res;
   uint8_t* aux;
   float* part;  // the tile's row of column sums (null: none)
@@ -173,7 +174,8 @@ __device__ __forceinline__ void apply_slopes(float (&x)[8], const float (&z)[8],
 // ---- eight consecutive columns of a row of C's type -----------------------------
 template <int DT> struct Row8 {
   static constexpr int OS = OutSize<DT>::v, W = OS / 2;
-  static constexpr int OT = DT == DT_FP8 ? DT_BF16 : DT;  // type of C
+  static constexpr int OT = DT == DT_FP8 || DT == DT_I8_BF16 ? DT_BF16
+                            : DT == DT_I8_F16 ? DT_F16 : DT == DT_I8_F32 ? DT_F32 : DT;  // type of C
   u32x4 w[W];
   // byte offset `off`; the first `left` columns lie inside the matrix (vec: all eight, or
   // `off` is out of range)
@@ -259,13 +261,39 @@ template <int DT> __device__ __forceinline__ f32x4 load_bias4(const EpiOut& o, i
     return b;
   }
 }
+// The scales of row i and of columns j .. j + 3 (products of 8-bit integers; reads past the
+// matrix return 0).
+template <int DT> __device__ __forceinline__ float row_scale(const EpiOut& o, int i) {
+  if constexpr (!IsInt8<DT>::v) return 1.0f;
+  else {
+    if (!o.row_scales) return 1.0f;
+    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(o.row_scales, o.m * 4), i * 4, 0, 0));
+  }
+}
+template <int DT> __device__ __forceinline__ f32x4 load_scales4(const EpiOut& o, int j) {
+  if constexpr (!IsInt8<DT>::v) return f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+  else {
+    if (!o.col_scales) return f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(o.col_scales, o.n * 4), j * 4, 0, 0));
+  }
+}
+// A sum of 8-bit integers' products, from its bits, times its scales, plus the bias.
+__device__ __forceinline__ float scaled_int(float bits, float rs, float cs, float b) {
+  return __builtin_fmaf((float)__builtin_bit_cast(int, bits) * rs, cs, b);
+}
 template <int DT> __device__ __forceinline__ f32x4 linear_sums(f32x4 x, float scale, f32x4 b) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) x[q] = DT == DT_FP8 ? __builtin_fmaf(x[q], scale, b[q]) : x[q] + b[q];
   return x;
 }
-template <int DT> __device__ __forceinline__ u32x2 linear4(f32x4 x, float scale, f32x4 b) {
-  x = linear_sums<DT>(x, scale, b);
+template <int DT>
+__device__ __forceinline__ u32x2 linear4(f32x4 x, float scale, f32x4 b, float rs, f32x4 cs) {
+  if constexpr (IsInt8<DT>::v) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = scaled_int(x[q], rs, cs[q], b[q]);
+  } else {
+    x = linear_sums<DT>(x, scale, b);
+  }
   return u32x2{to_out2<Row8<DT>::OT>(x[0], x[1]), to_out2<Row8<DT>::OT>(x[2], x[3])};
 }
 
@@ -288,6 +316,7 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
   bool grad;
   bool whole;     // every lane of the wave has all its columns inside C, or none
   float b[8], sum[8];
+  f32x4 cs[2];    // 8-bit integers: the columns' scales
 
   __device__ __forceinline__ EpiWave(const EpiOut& out, int lane_) : o(out), lane(lane_) {
     rc = make_rsrc(o.c, o.c_bytes);
@@ -301,6 +330,7 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
     left = o.n - col;
     whole = __ballot(left > 0 && left < 8) == 0;
     load_bias<DT>(o, col, b);
+    if constexpr (IsInt8<DT>::v) cs[0] = load_scales4<DT>(o, col), cs[1] = load_scales4<DT>(o, col + 4);
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum[q] = 0.0f;
   }
@@ -313,11 +343,15 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
     if (grad) aux.load(ra, at(in, row, o.ldaux), whole && (OS == 4 || o.aux_vec), left);
   }
 
-  // Eight sums of a row to C.
-  __device__ __forceinline__ void finish(bool in, int row, float (&x)[8], const Row8<DT>& res, const Row8<DT>& aux) {
+  // Eight sums of a row to C (rs: its row_scale()).
+  __device__ __forceinline__ void finish(bool in, int row, float (&x)[8], const Row8<DT>& res, const Row8<DT>& aux,
+                                         float rs) {
     Row8<DT> w;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) x[q] = DT == DT_FP8 ? __builtin_fmaf(x[q], o.scale, b[q]) : x[q] + b[q];
+    for (int q = 0; q < 8; ++q) {
+      if constexpr (IsInt8<DT>::v) x[q] = scaled_int(x[q], rs, cs[q / 4][q & 3], b[q]);
+      else x[q] = DT == DT_FP8 ? __builtin_fmaf(x[q], o.scale, b[q]) : x[q] + b[q];
+    }
     if (grad) {
       float z[8];
       aux.get(z);
@@ -353,9 +387,12 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
     for (int u0 = 0; u0 < PASSES; u0 += AHEAD) {
       Row8<DT> res[AHEAD], aux[AHEAD];
       const int r0 = lane / LPR + u0 * RP;
+      float rs[AHEAD];
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u)
+      for (int u = 0; u < AHEAD; ++u) {
         load_inputs(r0 + u * RP < count && left > 0, m0 + r0 + u * RP, res[u], aux[u]);
+        rs[u] = row_scale<DT>(o, m0 + r0 + u * RP);
+      }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         const int r = r0 + u * RP;
@@ -363,7 +400,7 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
         const f32x4 lo = *(const __attribute__((address_space(3))) f32x4*)p;
         const f32x4 hi = *(const __attribute__((address_space(3))) f32x4*)(p + 16);
         float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        finish(r < count && left > 0, m0 + r, x, res[u], aux[u]);
+        finish(r < count && left > 0, m0 + r, x, res[u], aux[u], rs[u]);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next block's sums
@@ -435,7 +472,7 @@ __global__ void __launch_bounds__(256) split_reduce_ep(KLaunch L, KEpis E) {
           if (q < x.left)
             for (int s = 0; s < S; ++s) v[q] += P[s * plane + q];
       }
-      x.finish(true, row, v, res, aux);
+      x.finish(true, row, v, res, aux, 1.0f);
     }
     if (x.o.part) {
       x.put_sums((lds_u8*)smem, tid / Wave::LPR, BN, (tid % Wave::LPR) * 8);

@@ -1,0 +1,400 @@
+// expert_operators.h -- host side of routing, scatter, combine, quantisation and products
+// of 8-bit integers: checks, tile choice, launches.  Part of gdy.cpp, behind operators.h.
+#pragma once
+
+namespace {
+
+// Leading dimensions whose byte offsets a 64-bit product holds for any row.
+bool good_ld(int64_t ld, int64_t n) { return ld >= n && ld <= kMaxStride; }
+
+bool row_type(int32_t t) { return t == GDY_F16 || t == GDY_BF16 || t == GDY_F32; }
+
+// Sizes of the operators by token.
+gdy_status check_tokens(gdy_ctx* ctx, const char* what, int64_t tokens, int64_t rows, int64_t n, int32_t top_k) {
+  if (tokens < 0 || rows < 0 || n < 0) return fail(ctx, GDY_ERR_INVALID_ARG, "%s: negative size", what);
+  if (top_k < 1 || top_k > GDY_MAX_TOP_K)
+    return fail(ctx, GDY_ERR_INVALID_ARG, "%s: top_k %d is not 1 to %d", what, top_k, GDY_MAX_TOP_K);
+  if (tokens > INT32_MAX - 4096 || rows > INT32_MAX - 4096 || n > INT32_MAX / 8)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "%s: sizes too large", what);
+  return GDY_OK;
+}
+
+// The weights of pairs: their type, place and range.
+gdy_status check_weights(gdy_ctx* ctx, const char* what, const void* weights, int32_t weights_type, int32_t type,
+                         int64_t pairs, std::vector<Range>* ranges) {
+  if (!weights) return GDY_OK;
+  if (weights_type != GDY_F32 && weights_type != type)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "%s: weights of type %d, rows of %d", what, weights_type, type);
+  const int ws = elem_size(weights_type);
+  if ((uintptr_t)weights % ws) return fail(ctx, GDY_ERR_UNSUPPORTED, "%s: weights not element aligned", what);
+  ranges->push_back({matrix_range(weights, 1, pairs, 0, 1, 0, ws), false, 0});
+  return GDY_OK;
+}
+
+// Threads that share a row of `units` pieces of work, as a power of two of at most kRowThreads.
+int row_threads_log(int64_t units) {
+  int l = 0;
+  while ((1 << l) < kRowThreads && (1 << l) < units) ++l;
+  return l;
+}
+
+// Workgroups for `rows` rows; kernels loop where 2^22 of them are not enough.
+unsigned row_grid(int64_t rows, int tpr_log) {
+  const int64_t per = kRowThreads >> tpr_log;
+  return (unsigned)std::min<int64_t>((rows + per - 1) / per, 1 << 22);
+}
+
+hipError_t launch_rows(const void* func, void* args, int64_t rows, int tpr_log, hipStream_t hs) {
+  void* argv[] = {args};
+  return hipExtLaunchKernel(func, dim3(row_grid(rows, tpr_log)), dim3(kRowThreads), argv, 0, hs, nullptr, nullptr, 0);
+}
+
+// ---------------------------------------------------------------------------
+// Routing
+// ---------------------------------------------------------------------------
+gdy_status validate_route(gdy_ctx* ctx, const gdy_route& g) {
+  if (g.tokens < 0 || g.experts < 0) return fail(ctx, GDY_ERR_INVALID_ARG, "route: negative size");
+  if (g.top_k < 1 || g.top_k > GDY_MAX_TOP_K)
+    return fail(ctx, GDY_ERR_INVALID_ARG, "route: top_k %d is not 1 to %d", g.top_k, GDY_MAX_TOP_K);
+  if (g.experts > GDY_MAX_GROUPS)
+    return fail(ctx, GDY_ERR_TOO_MANY, "route: %d experts > %d", g.experts, GDY_MAX_GROUPS);
+  if ((g.id_bytes != 4 && g.id_bytes != 8) || g.reserved != 0)
+    return fail(ctx, GDY_ERR_INVALID_ARG, "route: id_bytes must be 4 or 8, reserved 0");
+  if (g.tokens > ((int64_t)1 << 24) / g.top_k)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "route: more than 2^24 pairs");
+  if (!g.offsets || (uintptr_t)g.offsets % 4) return fail(ctx, GDY_ERR_INVALID_ARG, "route: null or unaligned offsets");
+  std::vector<Range> ranges;
+  ranges.push_back({matrix_range(g.offsets, 1, (int64_t)g.experts + 1, 0, 1, 0, 4), true, 0});
+  if (g.tokens > 0) {
+    if (!g.ids || !g.slots || (uintptr_t)g.slots % 4 || (uintptr_t)g.ids % g.id_bytes)
+      return fail(ctx, GDY_ERR_INVALID_ARG, "route: null or unaligned ids or slots");
+    if (!good_ld(g.ld_ids, g.top_k)) return fail(ctx, GDY_ERR_INVALID_ARG, "route: bad ld_ids");
+    ranges.push_back({matrix_range(g.ids, g.tokens, g.top_k, g.ld_ids, 1, 0, g.id_bytes), false, 0});
+    ranges.push_back({matrix_range(g.slots, 1, g.tokens * g.top_k, 0, 1, 0, 4), true, 0});
+  }
+  return check_ranges(ctx, ranges);
+}
+
+static_assert(GDY_MAX_GROUPS == kMaxExperts, "the kernels' tables hold every expert");
+
+gdy_status launch_route(gdy_ctx* ctx, const gdy_route& g, hipStream_t hs) {
+  KRoute a;
+  std::memset(&a, 0, sizeof a);
+  a.ids = g.ids;
+  a.slots = g.slots;
+  a.offsets = g.offsets;
+  a.ld_ids = g.ld_ids;
+  a.pairs = (int32_t)(g.tokens * g.top_k);
+  a.top_k = g.top_k;
+  a.experts = g.experts;
+  a.bits = ceil_log2((int64_t)g.experts + 1);
+  a.wide = g.id_bytes == 8;
+  a.dense = g.ld_ids == g.top_k || g.tokens <= 1;
+  const int most_parts = 128;
+  if (a.pairs <= GDY_ROUTE_ALONE) {
+    a.steps = std::max((a.pairs + kRoutePart - 1) / kRoutePart, 1);
+    a.parts = 1;
+  } else {
+    a.steps = std::min((a.pairs + kRoutePart * most_parts - 1) / (kRoutePart * most_parts), kRouteMaxSteps);
+    a.parts = (a.pairs + kRoutePart * a.steps - 1) / (kRoutePart * a.steps);
+    a.counts = (int32_t*)ctx->split_ws;  // at most 261 parts x 4096 experts
+  }
+  void* argv[] = {&a};
+  if (a.parts > 1)
+    HIP_TRY(ctx, hipExtLaunchKernel(route_count_kernel(), dim3(a.parts), dim3(kRoutePart), argv, 0, hs, nullptr, nullptr, 0));
+  HIP_TRY(ctx, hipExtLaunchKernel(route_slots_kernel(g.experts <= kRouteFew), dim3(a.parts), dim3(kRoutePart), argv, 0,
+                                  hs, nullptr, nullptr, 0));
+  return GDY_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Rows to the experts and back
+// ---------------------------------------------------------------------------
+gdy_status validate_scatter(gdy_ctx* ctx, const gdy_scatter& g) {
+  gdy_status s = check_tokens(ctx, "scatter", g.tokens, g.rows, g.n, g.top_k);
+  if (s != GDY_OK) return s;
+  if (!row_type(g.type) && !(g.type == GDY_FP8_E4M3 && !g.weights))
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "scatter: unsupported type %d", g.type);
+  if (g.reserved != 0) return fail(ctx, GDY_ERR_INVALID_ARG, "scatter: reserved must be 0");
+  if (g.weight_grad && !g.weights) return fail(ctx, GDY_ERR_INVALID_ARG, "scatter: weight_grad needs weights");
+  if (g.tokens == 0) return GDY_OK;
+  const int es = elem_size(g.type);
+  const int64_t pairs = g.tokens * g.top_k;
+  std::vector<Range> ranges;
+  if (!g.slots || (uintptr_t)g.slots % 4) return fail(ctx, GDY_ERR_INVALID_ARG, "scatter: null or unaligned slots");
+  ranges.push_back({matrix_range(g.slots, 1, pairs, 0, 1, 0, 4), false, 0});
+  s = check_weights(ctx, "scatter", g.weights, g.weights_type, g.type, pairs, &ranges);
+  if (s != GDY_OK) return s;
+  if ((uintptr_t)g.weight_grad % 4) return fail(ctx, GDY_ERR_UNSUPPORTED, "scatter: weight_grad not element aligned");
+  ranges.push_back({matrix_range(g.weight_grad, 1, pairs, 0, 1, 0, 4), true, 0});
+  if (g.n > 0 && g.rows > 0) {
+    if (!g.x || !g.out || (g.weight_grad && !g.z)) return fail(ctx, GDY_ERR_INVALID_ARG, "scatter: null x, out or z");
+    if (!good_ld(g.ldx, g.n) || !good_ld(g.ldo, g.n) || (g.weight_grad && !good_ld(g.ldz, g.n)))
+      return fail(ctx, GDY_ERR_INVALID_ARG, "scatter: a leading dimension < n or > 2^44");
+    if (((uintptr_t)g.x | (uintptr_t)g.out | (g.weight_grad ? (uintptr_t)g.z : 0)) % es)
+      return fail(ctx, GDY_ERR_UNSUPPORTED, "scatter: operands not element aligned");
+    ranges.push_back({matrix_range(g.x, g.tokens, g.n, g.ldx, 1, 0, es), false, 0});
+    ranges.push_back({matrix_range(g.out, g.rows, g.n, g.ldo, 1, 0, es), true, 0});
+    if (g.weight_grad) ranges.push_back({matrix_range(g.z, g.rows, g.n, g.ldz, 1, 0, es), false, 0});
+  }
+  return check_ranges(ctx, ranges);
+}
+
+gdy_status launch_scatter(gdy_ctx* ctx, const gdy_scatter& g, hipStream_t hs) {
+  // without rows or columns there is nothing to move; weight_grad is zeros
+  const bool moves = g.n > 0 && g.rows > 0;
+  if (g.tokens == 0 || (!moves && !g.weight_grad)) return GDY_OK;
+  const int es = elem_size(g.type);
+  KScatter a;
+  std::memset(&a, 0, sizeof a);
+  a.x = (const uint8_t*)g.x;
+  a.out = (uint8_t*)g.out;
+  a.z = (const uint8_t*)g.z;
+  a.slots = g.slots;
+  a.weights = g.weights;
+  a.weight_grad = g.weight_grad;
+  a.tokens = g.tokens;
+  a.ldx = g.ldx * es;
+  a.ldo = g.ldo * es;
+  a.ldz = g.ldz * es;
+  a.rows = moves ? (int32_t)g.rows : 0;
+  a.n = moves ? (int32_t)g.n : 0;
+  a.top_k = g.top_k;
+  a.weights_f32 = g.weights_type == GDY_F32;
+  a.tpr_log = row_threads_log(((int64_t)a.n * es + 15) / 16);
+  HIP_TRY(ctx, launch_rows(scatter_kernel(g.type, g.weight_grad ? 2 : g.weights ? 1 : 0), &a, g.tokens, a.tpr_log, hs));
+  return GDY_OK;
+}
+
+gdy_status validate_combine(gdy_ctx* ctx, const gdy_combine& g) {
+  gdy_status s = check_tokens(ctx, "combine", g.tokens, g.rows, g.n, g.top_k);
+  if (s != GDY_OK) return s;
+  if (!row_type(g.type)) return fail(ctx, GDY_ERR_UNSUPPORTED, "combine: unsupported type %d", g.type);
+  if (g.reserved != 0) return fail(ctx, GDY_ERR_INVALID_ARG, "combine: reserved must be 0");
+  if (g.tokens == 0 || g.n == 0) return GDY_OK;
+  const int es = elem_size(g.type);
+  const int64_t pairs = g.tokens * g.top_k;
+  std::vector<Range> ranges;
+  if (!g.slots || (uintptr_t)g.slots % 4) return fail(ctx, GDY_ERR_INVALID_ARG, "combine: null or unaligned slots");
+  ranges.push_back({matrix_range(g.slots, 1, pairs, 0, 1, 0, 4), false, 0});
+  s = check_weights(ctx, "combine", g.weights, g.weights_type, g.type, pairs, &ranges);
+  if (s != GDY_OK) return s;
+  if (!g.y || (g.rows > 0 && !g.z)) return fail(ctx, GDY_ERR_INVALID_ARG, "combine: null y or z");
+  if (!good_ld(g.ldy, g.n) || (g.rows > 0 && !good_ld(g.ldz, g.n)) || (g.residual && !good_ld(g.ldr, g.n)))
+    return fail(ctx, GDY_ERR_INVALID_ARG, "combine: a leading dimension < n or > 2^44");
+  if (((uintptr_t)g.y | (uintptr_t)g.residual | (g.rows > 0 ? (uintptr_t)g.z : 0)) % es)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "combine: operands not element aligned");
+  ranges.push_back({matrix_range(g.y, g.tokens, g.n, g.ldy, 1, 0, es), true, 1});
+  ranges.push_back({matrix_range(g.residual, g.tokens, g.n, g.ldr, 1, 0, es), false,
+                    g.residual == g.y && g.ldr == g.ldy ? 1 : 0});
+  if (g.rows > 0) ranges.push_back({matrix_range(g.z, g.rows, g.n, g.ldz, 1, 0, es), false, 0});
+  return check_ranges(ctx, ranges);
+}
+
+gdy_status launch_combine(gdy_ctx* ctx, const gdy_combine& g, hipStream_t hs) {
+  if (g.tokens == 0 || g.n == 0) return GDY_OK;
+  const int es = elem_size(g.type);
+  KCombine a;
+  std::memset(&a, 0, sizeof a);
+  a.z = (const uint8_t*)g.z;
+  a.res = (const uint8_t*)g.residual;
+  a.y = (uint8_t*)g.y;
+  a.slots = g.slots;
+  a.weights = g.weights;
+  a.tokens = g.tokens;
+  a.ldz = g.ldz * es;
+  a.ldr = g.ldr * es;
+  a.ldy = g.ldy * es;
+  a.rows = (int32_t)g.rows;
+  a.n = (int32_t)g.n;
+  a.top_k = g.top_k;
+  a.weights_f32 = g.weights_type == GDY_F32;
+  a.tpr_log = row_threads_log((g.n * es + 15) / 16);
+  HIP_TRY(ctx, launch_rows(combine_kernel(g.type), &a, g.tokens, a.tpr_log, hs));
+  return GDY_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Rows to 8-bit integers
+// ---------------------------------------------------------------------------
+gdy_status validate_quantize(gdy_ctx* ctx, const gdy_quantize& g) {
+  if (!g.slots && (g.top_k != 0 || g.out_rows != 0))
+    return fail(ctx, GDY_ERR_INVALID_ARG, "quantize: top_k and out_rows belong to slots, 0 without them");
+  const gdy_status s = check_tokens(ctx, "quantize", g.rows, g.out_rows, g.n, g.slots ? g.top_k : 1);
+  if (s != GDY_OK) return s;
+  if (!row_type(g.type)) return fail(ctx, GDY_ERR_UNSUPPORTED, "quantize: unsupported type %d", g.type);
+  const int64_t out_rows = g.slots ? g.out_rows : g.rows;
+  if (g.rows == 0 || out_rows == 0) return GDY_OK;
+  const int es = elem_size(g.type);
+  if ((uintptr_t)g.slots % 4 || !g.scales || (uintptr_t)g.scales % 4)
+    return fail(ctx, GDY_ERR_INVALID_ARG, "quantize: unaligned slots, null or unaligned scales");
+  std::vector<Range> ranges;
+  ranges.push_back({matrix_range(g.slots, 1, g.rows * g.top_k, 0, 1, 0, 4), false, 0});
+  ranges.push_back({matrix_range(g.scales, 1, out_rows, 0, 1, 0, 4), true, 0});
+  if (g.n > 0) {
+    if (!g.x || !g.q) return fail(ctx, GDY_ERR_INVALID_ARG, "quantize: null x or q");
+    if (!good_ld(g.ldx, g.n) || !good_ld(g.ldq, g.n))
+      return fail(ctx, GDY_ERR_INVALID_ARG, "quantize: a leading dimension < n or > 2^44");
+    if ((uintptr_t)g.x % es) return fail(ctx, GDY_ERR_UNSUPPORTED, "quantize: x not element aligned");
+    ranges.push_back({matrix_range(g.x, g.rows, g.n, g.ldx, 1, 0, es), false, 0});
+    ranges.push_back({matrix_range(g.q, out_rows, g.n, g.ldq, 1, 0, 1), true, 0});
+  }
+  return check_ranges(ctx, ranges);
+}
+
+gdy_status launch_quantize(gdy_ctx* ctx, const gdy_quantize& g, hipStream_t hs) {
+  if (g.rows == 0 || (g.slots && g.out_rows == 0)) return GDY_OK;
+  KQuantize a;
+  std::memset(&a, 0, sizeof a);
+  a.x = (const uint8_t*)g.x;
+  a.q = g.q;
+  a.scales = g.scales;
+  a.slots = g.slots;
+  a.rows = g.rows;
+  a.ldx = g.ldx * elem_size(g.type);
+  a.ldq = g.ldq;
+  a.n = (int32_t)g.n;
+  a.top_k = g.top_k;
+  a.out_rows = (int32_t)g.out_rows;
+  a.tpr_log = row_threads_log((g.n + 15) / 16);
+  HIP_TRY(ctx, launch_rows(quantize_kernel(g.type), &a, g.rows, a.tpr_log, hs));
+  return GDY_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Products of 8-bit integers
+// ---------------------------------------------------------------------------
+const int64_t kMaxIntegerK = 131071;  // k * 128 * 128 < 2^31
+
+gdy_status validate_integer(gdy_ctx* ctx, const gdy_integer& g, const gdy_epilogue* ep) {
+  const bool grouped = g.offsets != nullptr;
+  if (g.rows < 0 || g.n < 0 || g.k < 0 || (grouped && g.groups < 0))
+    return fail(ctx, GDY_ERR_INVALID_ARG, "integer: negative size");
+  if (grouped && g.groups > GDY_MAX_GROUPS)
+    return fail(ctx, GDY_ERR_TOO_MANY, "integer: %d groups > %d", g.groups, GDY_MAX_GROUPS);
+  if (!row_type(g.c_type)) return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: unsupported type %d of C", g.c_type);
+  if ((g.trans_b != 0 && g.trans_b != 1) || g.reserved != 0)
+    return fail(ctx, GDY_ERR_INVALID_ARG, "integer: trans_b must be 0 or 1, reserved 0");
+  if (g.k > kMaxIntegerK)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: k %lld > %lld, whose sums may pass 32 bits", (long long)g.k,
+                (long long)kMaxIntegerK);
+  if (ep && (ep->grad || ep->aux || ep->bias_grad))
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: the epilogue may hold a bias, an activation and a residual only");
+  const int64_t groups = grouped ? g.groups : 1;
+  if (groups == 0 || g.rows == 0 || g.n == 0) return GDY_OK;
+  // sizes are 32-bit on the device, row tiles and their columns one 31-bit count
+  if (g.rows > INT32_MAX - 4096 || g.n > INT32_MAX - 4096 ||
+      ((g.rows + 15) / 16 + groups) * ((g.n + 15) / 16) > INT32_MAX / 2)
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: sizes too large");
+  if ((uintptr_t)g.offsets % 4 || (uintptr_t)g.row_scales % 4 || (uintptr_t)g.col_scales % 4)
+    return fail(ctx, GDY_ERR_INVALID_ARG, "integer: unaligned offsets or scales");
+  const int os = g.c_type == GDY_F32 ? 4 : 2;
+  if (!g.c) return fail(ctx, GDY_ERR_INVALID_ARG, "integer: null C");
+  if (g.ldc < g.n) return fail(ctx, GDY_ERR_INVALID_ARG, "integer: ldc < n");
+  if ((uintptr_t)g.c % os) return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: C not element aligned");
+  int64_t bytes;
+  const int64_t tile_rows = std::min<int64_t>(g.rows, 256);
+  if (!stored_extent(tile_rows, g.n, g.ldc, os, &bytes))
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: rows of C too long");
+  const bool many = groups > 1;
+  if (many && g.col_scales && (g.stride_col_scales < 0 || (g.stride_col_scales > 0 && g.stride_col_scales < g.n)))
+    return fail(ctx, GDY_ERR_INVALID_ARG, "integer: bad stride_col_scales");
+  if (many && ((g.col_scales && g.stride_col_scales > kMaxStride) || g.stride_b > kMaxStride))
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: stride too large");
+  std::vector<Range> ranges;
+  ranges.push_back({matrix_range(g.offsets, 1, groups + 1, 0, 1, 0, 4), false, 0});
+  ranges.push_back({matrix_range(g.row_scales, 1, g.rows, 0, 1, 0, 4), false, 0});
+  ranges.push_back({matrix_range(g.col_scales, 1, g.n, 0, groups, many ? g.stride_col_scales : 0, 4), false, 0});
+  ranges.push_back({matrix_range(g.c, g.rows, g.n, g.ldc, 1, 0, os), true, 1});
+  if (g.k > 0) {
+    if (!g.a || !g.b) return fail(ctx, GDY_ERR_INVALID_ARG, "integer: null A or B");
+    if (g.lda < g.k || g.ldb < (g.trans_b ? g.k : g.n))
+      return fail(ctx, GDY_ERR_INVALID_ARG, "integer: lda or ldb too small");
+    if (many && g.stride_b < 0) return fail(ctx, GDY_ERR_INVALID_ARG, "integer: negative stride_b");
+    const int64_t br = g.trans_b ? g.n : g.k, bc = g.trans_b ? g.k : g.n;
+    if (!stored_extent(tile_rows, g.k, g.lda, 1, &bytes) || !stored_extent(br, bc, g.ldb, 1, &bytes))
+      return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: A or B extent too large");
+    ranges.push_back({matrix_range(g.a, g.rows, g.k, g.lda, 1, 0, 1), false, 0});
+    ranges.push_back({matrix_range(g.b, br, bc, g.ldb, groups, many ? g.stride_b : 0, 1), false, 0});
+  }
+  if (ep) {
+    const EpiTarget t = {"integer", 0, g.c, g.rows, g.n, g.ldc, -1, 1, groups, g.c_type, 1};
+    const gdy_status s = validate_epilogue(ctx, *ep, t, &ranges);
+    if (s != GDY_OK) return s;
+  }
+  return check_ranges(ctx, ranges);
+}
+
+gdy_status launch_integer(gdy_ctx* ctx, const gdy_integer& g, const gdy_epilogue* ep, hipStream_t hs) {
+  const bool grouped = g.offsets != nullptr;
+  const int groups = grouped ? g.groups : 1;
+  if (groups == 0 || g.rows == 0 || g.n == 0) return GDY_OK;
+  const int os = g.c_type == GDY_F32 ? 4 : 2;
+  const bool many = groups > 1;
+  KInteger q;
+  std::memset(&q, 0, sizeof q);
+  q.row_scales = g.row_scales;
+  q.col_scales = g.col_scales;
+  q.stride_col_scales = many ? g.stride_col_scales : 0;
+  KGroup& a = q.g;
+  a.a = (const uint8_t*)g.a;
+  a.b = (const uint8_t*)g.b;
+  a.c = (uint8_t*)g.c;
+  a.offsets = g.offsets;
+  a.stride_b = many ? g.stride_b : 0;
+  a.rows = a.m = (int32_t)g.rows;
+  a.groups = groups;
+  a.n = (int32_t)g.n;
+  a.k = (int32_t)g.k;
+  a.lda = (int32_t)g.lda;
+  a.ldb = (int32_t)g.ldb;
+  a.ldc = (int32_t)g.ldc;
+  a.scale = 1.0f;
+  auto vec = [&](const void* p, int64_t ld) { return (uintptr_t)p % 8 == 0 && (ld * os) % 8 == 0; };
+  a.c_vec = vec(g.c, g.ldc);
+  a.a_dma = copies_ok(g.a, g.lda, g.k, 1, true, 0);
+  a.b_dma = copies_ok(g.b, g.ldb, g.k, 1, g.trans_b != 0, a.stride_b);
+  a.xcd_cus = std::max(ctx->cus / kXcds, 1);
+  if (ep) {
+    a.epi.bias = (const uint8_t*)ep->bias;
+    a.epi.bias_f32 = ep->bias && ep->bias_type == GDY_F32;
+    a.epi.stride_bias = many ? ep->stride_bias * (a.epi.bias_f32 ? 4 : os) : 0;
+    a.epi.res = (const uint8_t*)ep->residual;
+    a.epi.ldr = (int32_t)ep->ldr;
+    a.epi.res_vec = vec(ep->residual, ep->ldr);
+    a.epi.act = ep->act;
+  }
+  // the tile of the fp8 product of these sizes
+  gdy_grouped like;
+  std::memset(&like, 0, sizeof like);
+  like.a_type = like.b_type = GDY_FP8_E4M3;
+  like.groups = groups;
+  like.rows = g.rows;
+  like.n = g.n;
+  like.k = g.k;
+  like.trans_b = g.trans_b;
+  const bool copies = a.a_dma && a.b_dma;
+  auto kernel = [&](int tile, bool few) {
+    return g.c_type == GDY_BF16 ? integer_bf16(g.trans_b, tile, few)
+           : g.c_type == GDY_F16 ? integer_f16(g.trans_b, tile, few) : integer_f32(g.trans_b, tile, few);
+  };
+  GroupKernel kern;
+  if (g.trans_b && group_rows_few(like, copies)) {
+    kern = kernel(0, true);
+    a.bm = kern.bm;
+  } else {
+    const GroupTileCost& tile = group_rows_tile(ctx, like, copies);
+    kern = kernel(tile.tile, false);
+    a.bm = tile.bm;
+  }
+  a.max_slots = (int32_t)(grouped ? max_row_tiles(g.rows, groups, a.bm) : (g.rows + a.bm - 1) / a.bm);
+  const int64_t tn = (g.n + kern.bn - 1) / kern.bn;
+  const int64_t grid = (((int64_t)a.max_slots * tn + kXcds - 1) / kXcds + a.xcd_cus / 2) * kXcds;
+  if (grid * kern.threads > UINT32_MAX)  // threads of a launch
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: a grid of %lld workgroups", (long long)grid);
+  void* argv[] = {&q};
+  HIP_TRY(ctx, hipExtLaunchKernel(kern.func, dim3((unsigned)grid), dim3(kern.threads), argv, 0, hs, nullptr, nullptr, 0));
+  return GDY_OK;
+}
+
+}  // namespace

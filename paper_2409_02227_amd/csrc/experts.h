@@ -1,0 +1,267 @@
+// experts.h -- what a mixture of experts does around its grouped products: the rows of
+// each expert (route), tokens' rows to them (scatter) and back (combine), with the
+// gradients of both.
+//
+// Scatter and combine are bound by memory.  Both go by tokens: a token's row is read (or
+// written) once and its top_k rows of the other side next to it, so that nothing but the
+// slots says where rows lie, no atomics are needed and every sum has a fixed order.
+#pragma once
+#include "grouped.h"
+#include "rows.h"
+
+namespace gdy {
+
+// The weight of a pair.
+template <int DT> __device__ __forceinline__ float pair_weight(const void* weights, bool f32, int64_t pair) {
+  if (f32) return ((const float*)weights)[pair];
+  if constexpr (ElemSize<DT>::v == 2) return ew_decode<DT>(((const uint16_t*)weights)[pair]);
+  else return ((const float*)weights)[pair];
+}
+
+// ---- rows to the experts ---------------------------------------------------------
+// MODE 0: copies, 1: weighted, 2: weighted, with the gradient of the weights.
+template <int DT, int MODE>
+__global__ void __launch_bounds__(kRowThreads) scatter_rows(KScatter g) {
+  typedef RowChunk<DT> C;
+  constexpr int JU = 4;  // pairs of a token that are under way together
+  __shared__ float lds[MODE == 2 ? kRowThreads / 64 * JU : 1];
+  const RowPlace at(g.tpr_log);
+  const int step = 1 << g.tpr_log, n = g.n;
+  for (int64_t t0 = (int64_t)blockIdx.x * at.rows; t0 < g.tokens; t0 += (int64_t)gridDim.x * at.rows) {
+    const int64_t t = t0 + at.sub;
+    const bool live = t < g.tokens;
+    const uint8_t* x = g.x + (live ? t : 0) * g.ldx;
+    for (int j0 = 0; j0 < g.top_k; j0 += JU) {
+      int slot[JU];
+      float w[JU], dot[JU];
+#pragma unroll
+      for (int u = 0; u < JU; ++u) {
+        const int64_t pair = t * g.top_k + j0 + u;
+        const bool in = live && j0 + u < g.top_k;
+        slot[u] = in ? g.slots[pair] : -1;
+        if ((unsigned)slot[u] >= (unsigned)g.rows) slot[u] = -1;
+        w[u] = MODE && in ? pair_weight<DT>(g.weights, g.weights_f32, pair) : 1.0f;
+        dot[u] = 0.0f;
+      }
+      for (int c = at.lane * C::VN; c < n; c += step * C::VN) {
+        if (!live) break;
+        const int left = n - c;
+        C v, z[JU];
+        v.load(x + (int64_t)c * C::ES, left);
+        if (MODE == 2 && g.rows > 0) {
+#pragma unroll
+          for (int u = 0; u < JU; ++u)  // pairs without a row read one that is there
+            z[u].load(g.z + max(slot[u], 0) * g.ldz + (int64_t)c * C::ES, left);
+        }
+#pragma unroll
+        for (int u = 0; u < JU; ++u) {
+          if (slot[u] < 0) continue;
+          C o = v;
+          if constexpr (MODE != 0) {
+            float y[C::VN];
+#pragma unroll
+            for (int e = 0; e < C::VN; ++e) {
+              y[e] = v.get(e) * w[u];
+              if (MODE == 2) dot[u] = __builtin_fmaf(v.get(e), z[u].get(e), dot[u]);
+            }
+            o.set(y);
+          }
+          o.store(g.out + slot[u] * g.ldo + (int64_t)c * C::ES, left);
+        }
+      }
+      if constexpr (MODE == 2) {
+        // the row's threads in a fixed order: halves of a wave's lanes, then its waves
+#pragma unroll
+        for (int u = 0; u < JU; ++u)
+          for (int d = 1; d < min(step, 64); d <<= 1) dot[u] += __shfl_xor(dot[u], d);
+        const int wave = (int)threadIdx.x >> 6;
+        if (step > 64) {
+          if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int u = 0; u < JU; ++u) lds[wave * JU + u] = dot[u];
+          __syncthreads();
+          if (at.lane == 0)
+#pragma unroll
+            for (int u = 0; u < JU; ++u)
+              for (int q = 1; q < step / 64; ++q) dot[u] += lds[(wave + q) * JU + u];
+          __syncthreads();
+        }
+        if (live && at.lane == 0)
+#pragma unroll
+          for (int u = 0; u < JU; ++u)
+            if (j0 + u < g.top_k) g.weight_grad[t * g.top_k + j0 + u] = slot[u] < 0 ? 0.0f : dot[u];
+      }
+    }
+  }
+}
+
+// ---- rows back from them ------------------------------------------------------------
+template <int DT>
+__global__ void __launch_bounds__(kRowThreads) combine_rows(KCombine g) {
+  typedef RowChunk<DT> C;
+  constexpr int JU = 4;
+  const RowPlace at(g.tpr_log);
+  const int step = 1 << g.tpr_log, n = g.n;
+  for (int64_t t = (int64_t)blockIdx.x * at.rows + at.sub; t < g.tokens; t += (int64_t)gridDim.x * at.rows) {
+    for (int c = at.lane * C::VN; c < n; c += step * C::VN) {
+      const int left = n - c;
+      float acc[C::VN];
+#pragma unroll
+      for (int e = 0; e < C::VN; ++e) acc[e] = 0.0f;
+      C r;
+      if (g.res) r.load(g.res + t * g.ldr + (int64_t)c * C::ES, left);
+      for (int j0 = 0; g.rows > 0 && j0 < g.top_k; j0 += JU) {
+        int slot[JU];
+        float w[JU];
+        C z[JU];
+#pragma unroll
+        for (int u = 0; u < JU; ++u) {
+          const int64_t pair = t * g.top_k + min(j0 + u, g.top_k - 1);
+          slot[u] = j0 + u < g.top_k ? g.slots[pair] : -1;
+          if ((unsigned)slot[u] >= (unsigned)g.rows) slot[u] = -1;
+          w[u] = g.weights ? pair_weight<DT>(g.weights, g.weights_f32, pair) : 1.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < JU; ++u)  // pairs without a row read one that is there
+          z[u].load(g.z + max(slot[u], 0) * g.ldz + (int64_t)c * C::ES, left);
+#pragma unroll
+        for (int u = 0; u < JU; ++u) {
+          if (slot[u] < 0) continue;
+#pragma unroll
+          for (int e = 0; e < C::VN; ++e) acc[e] = __builtin_fmaf(w[u], z[u].get(e), acc[e]);
+        }
+      }
+      if (g.res) {
+#pragma unroll
+        for (int e = 0; e < C::VN; ++e) acc[e] += r.get(e);
+      }
+      C o;
+      o.set(acc);
+      o.store(g.y + t * g.ldy + (int64_t)c * C::ES, left);
+    }
+  }
+}
+
+// ---- the rows of each expert -----------------------------------------------------------
+// A stable sort by counting.  Its parts are kRoutePart * `steps` consecutive pairs each, a
+// workgroup's; a wave takes consecutive pairs, 64 a step, so that the pairs before one are those
+// of the parts before, of the waves before, and of the wave's own steps and lanes before.
+// Within a step the lanes of one expert find each other by a ballot for each bit of the id.
+// All counts are integers: no order of additions matters.
+constexpr int kRouteWaves = kRoutePart / 64;
+
+// The expert of pair p (`experts`: none).
+__device__ __forceinline__ int pair_expert(const KRoute& g, int p) {
+  if (p >= g.pairs) return g.experts;
+  int64_t at = p;
+  if (!g.dense) {
+    const int t = p / g.top_k;
+    at = t * g.ld_ids + (p - t * g.top_k);
+  }
+  const int64_t id = g.wide ? ((const int64_t*)g.ids)[at] : ((const int32_t*)g.ids)[at];
+  return id >= 0 && id < g.experts ? (int)id : g.experts;
+}
+
+// The lanes of the wave whose expert is this lane's.
+__device__ __forceinline__ uint64_t same_expert(int e, int bits) {
+  uint64_t m = ~0ull;
+  for (int b = 0; b < bits; ++b) {
+    const bool on = (e >> b) & 1;
+    const uint64_t has = __ballot(on);
+    m &= on ? has : ~has;
+  }
+  return m;
+}
+
+// Pairs of each expert in every part: counts[part][expert].
+__global__ void __launch_bounds__(kRoutePart) route_count(KRoute g) {
+  __shared__ int hist[kMaxExperts];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int e = tid; e < g.experts; e += kRoutePart) hist[e] = 0;
+  __syncthreads();
+  const int p0 = ((int)blockIdx.x * kRouteWaves + wave) * g.steps * 64 + lane;
+  for (int s = 0; s < g.steps; ++s) {
+    const int e = pair_expert(g, p0 + s * 64);
+    const uint64_t m = same_expert(e, g.bits);
+    if (e < g.experts && lane == (int)__builtin_ctzll(m)) atomicAdd(&hist[e], (int)__builtin_popcountll(m));
+  }
+  __syncthreads();
+  for (int e = tid; e < g.experts; e += kRoutePart) g.counts[(int64_t)blockIdx.x * g.experts + e] = hist[e];
+}
+
+// Slots of a part's pairs, and (the first part) the offsets.  parts == 1: this kernel alone.
+// Counts of a wave and expert are 16 bits: a part has fewer than 2^16 pairs.
+template <int EXPERTS>
+__global__ void __launch_bounds__(kRoutePart) route_slots(KRoute g) {
+  __shared__ int base[EXPERTS];
+  __shared__ uint16_t count[kRouteWaves][EXPERTS];
+  __shared__ int sums[kRouteWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int E = g.experts;
+  for (int e = tid; e < E; e += kRoutePart)
+#pragma unroll
+    for (int w = 0; w < kRouteWaves; ++w) count[w][e] = 0;
+  __syncthreads();
+  const int p0 = ((int)blockIdx.x * kRouteWaves + wave) * g.steps * 64 + lane;
+  // a step's pairs: their rank among the wave's pairs of their expert, on top of `count`
+  auto rank = [&](int e) {
+    const uint64_t m = same_expert(e, g.bits);
+    int r = 0;
+    if (e < E) {
+      const int before = count[wave][e];  // read by all lanes of the expert, then written by the first
+      r = before + (int)__builtin_popcountll(m & ((1ull << lane) - 1));
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      if (lane == (int)__builtin_ctzll(m)) count[wave][e] = (uint16_t)(before + (int)__builtin_popcountll(m));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next step's reads
+    __builtin_amdgcn_wave_barrier();
+    return r;
+  };
+  for (int s = 0; s < g.steps; ++s) rank(pair_expert(g, p0 + s * 64));
+  __syncthreads();
+  // experts, kRoutePart at a time: counts of the waves before, of the parts before, of the experts before
+  int below = 0;
+  for (int e0 = 0; e0 < E; e0 += kRoutePart) {
+    const int e = e0 + tid;
+    int total = 0, before = 0;
+    if (e < E) {
+#pragma unroll
+      for (int w = 0; w < kRouteWaves; ++w) {
+        const int c = count[w][e];
+        count[w][e] = (uint16_t)total;
+        total += c;
+      }
+      if (g.parts > 1) {
+        total = 0;
+#pragma unroll 8
+        for (int q = 0; q < g.parts; ++q) {
+          const int c = g.counts[(int64_t)q * E + e];
+          before += q < (int)blockIdx.x ? c : 0;
+          total += c;
+        }
+      }
+    }
+    const int upto = wave_scan(total);  // of the wave's experts, this one among them
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int first = below + upto - total;
+    for (int w = 0; w < kRouteWaves; ++w) {
+      if (w < wave) first += sums[w];
+      below += sums[w];
+    }
+    if (e < E) {
+      base[e] = first + before;
+      if (blockIdx.x == 0) g.offsets[e] = first;
+    }
+    __syncthreads();
+  }
+  if (blockIdx.x == 0 && tid == 0) g.offsets[E] = below;
+  for (int s = 0; s < g.steps; ++s) {
+    const int p = p0 + s * 64, e = pair_expert(g, p);
+    const int r = rank(e);
+    if (p < g.pairs) g.slots[p] = e < E ? base[e] + r : -1;
+  }
+}
+
+}  // namespace gdy

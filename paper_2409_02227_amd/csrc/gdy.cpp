@@ -2333,6 +2333,7 @@ gdy_status load_table(gdy_ctx* ctx, const char* path) {
 // C-ABI
 // ---------------------------------------------------------------------------
 #include "operators.h"
+#include "expert_operators.h"
 
 extern "C" {
 
@@ -2763,6 +2764,61 @@ gdy_status gdy_execute_act_grad(gdy_ctx* ctx, const gdy_act_grad* op, void* hip_
     DeviceGuard guard;
     HIP_TRY(ctx, guard.enter(ctx->device));
     return launch_act_grad(ctx, *op, (hipStream_t)hip_stream);
+  } catch (...) {
+    return fail(ctx, GDY_ERR_NOMEM, "host allocation failed");
+  }
+}
+
+extern "C++" {
+// A call of an operator that takes no epilogue: checked, then launched on the context's device.
+template <class Op>
+static gdy_status execute_operator(gdy_ctx* ctx, const Op* op, void* hip_stream,
+                                   gdy_status (*check)(gdy_ctx*, const Op&),
+                                   gdy_status (*launch)(gdy_ctx*, const Op&, hipStream_t)) {
+  if (!ctx) return GDY_ERR_INVALID_ARG;
+  ctx->err.clear();
+  try {
+    if (!op) return fail(ctx, GDY_ERR_INVALID_ARG, "null operator");
+    const gdy_status s = check(ctx, *op);
+    if (s != GDY_OK) return s;
+    if (ctx->device < 0) return fail(ctx, GDY_ERR_UNSUPPORTED, "host-only context cannot execute");
+    DeviceGuard guard;
+    HIP_TRY(ctx, guard.enter(ctx->device));
+    return launch(ctx, *op, (hipStream_t)hip_stream);
+  } catch (...) {
+    return fail(ctx, GDY_ERR_NOMEM, "host allocation failed");
+  }
+}
+}
+
+gdy_status gdy_execute_route(gdy_ctx* ctx, const gdy_route* op, void* hip_stream) {
+  return execute_operator(ctx, op, hip_stream, validate_route, launch_route);
+}
+
+gdy_status gdy_execute_scatter(gdy_ctx* ctx, const gdy_scatter* op, void* hip_stream) {
+  return execute_operator(ctx, op, hip_stream, validate_scatter, launch_scatter);
+}
+
+gdy_status gdy_execute_combine(gdy_ctx* ctx, const gdy_combine* op, void* hip_stream) {
+  return execute_operator(ctx, op, hip_stream, validate_combine, launch_combine);
+}
+
+gdy_status gdy_execute_quantize(gdy_ctx* ctx, const gdy_quantize* op, void* hip_stream) {
+  return execute_operator(ctx, op, hip_stream, validate_quantize, launch_quantize);
+}
+
+gdy_status gdy_execute_integer(gdy_ctx* ctx, const gdy_integer* product, const gdy_epilogue* epilogue,
+                               void* hip_stream) {
+  if (!ctx) return GDY_ERR_INVALID_ARG;
+  ctx->err.clear();
+  try {
+    if (!product) return fail(ctx, GDY_ERR_INVALID_ARG, "null product");
+    const gdy_status s = validate_integer(ctx, *product, epilogue);
+    if (s != GDY_OK) return s;
+    if (ctx->device < 0) return fail(ctx, GDY_ERR_UNSUPPORTED, "host-only context cannot execute");
+    DeviceGuard guard;
+    HIP_TRY(ctx, guard.enter(ctx->device));
+    return launch_integer(ctx, *product, epilogue, (hipStream_t)hip_stream);
   } catch (...) {
     return fail(ctx, GDY_ERR_NOMEM, "host allocation failed");
   }

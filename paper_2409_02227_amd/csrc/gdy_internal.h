@@ -8,6 +8,8 @@ namespace gdy {
 
 // Element types, numerically equal to the public gdy_dtype values.
 enum : int { DT_F16 = 1, DT_BF16 = 2, DT_FP8 = 3, DT_F32 = 4 };
+// Products of 8-bit integers (integer.h), by the type of C; inside the library only.
+enum : int { DT_I8_F16 = 5, DT_I8_BF16 = 6, DT_I8_F32 = 7 };
 
 // Kernel arguments, passed by value.  Sizes and leading dimensions are in
 // elements; the storage reading is row-major with op(A)(i,k) = A[i*lda+k]
@@ -198,6 +200,65 @@ struct KActGrad {
 
 constexpr int kActCols = 512, kActRows = 32, kActThreads = 512;  // of a workgroup
 
+// Rows to the experts and back (experts.h).  Pitches are bytes.
+constexpr int kRowThreads = 256;  // of a workgroup
+struct KScatter {
+  const uint8_t* x;
+  uint8_t* out;
+  const uint8_t* z;        // read for weight_grad
+  const int32_t* slots;
+  const void* weights;
+  float* weight_grad;
+  int64_t tokens, ldx, ldo, ldz;
+  int32_t rows, n, top_k;
+  int32_t weights_f32;     // 1: weights are fp32, else of the rows' type
+  int32_t tpr_log;         // threads of a row: 1 << tpr_log
+};
+struct KCombine {
+  const uint8_t* z;
+  const uint8_t* res;      // null: none; may be y
+  uint8_t* y;
+  const int32_t* slots;
+  const void* weights;     // null: 1
+  int64_t tokens, ldz, ldr, ldy;
+  int32_t rows, n, top_k, weights_f32, tpr_log;
+};
+
+// The rows of each expert: parts of kRoutePart * steps pairs, a workgroup of kRoutePart
+// threads each.
+constexpr int kRoutePart = 1024, kRouteFew = 256, kMaxExperts = 4096;
+constexpr int kRouteMaxSteps = 63;  // parts of fewer than 2^16 pairs
+struct KRoute {
+  const void* ids;
+  int32_t* slots;
+  int32_t* offsets;
+  int32_t* counts;         // parts x experts
+  int64_t ld_ids;
+  int32_t pairs, top_k, experts;
+  int32_t bits;            // of the numbers 0 .. experts
+  int32_t wide, dense;     // 64-bit ids; ld_ids == top_k
+  int32_t steps, parts;
+};
+
+// Rows to 8-bit integers (quantize.h).  Pitches are bytes.
+struct KQuantize {
+  const uint8_t* x;
+  int8_t* q;
+  float* scales;
+  const int32_t* slots;    // null: row i to row i
+  int64_t rows, ldx, ldq;
+  int32_t n, top_k, out_rows, tpr_log;
+};
+
+// A product of 8-bit integers (integer.h): the grouped product (offsets null: one group of
+// all rows) and its scales.
+struct KInteger {
+  KGroup g;
+  const float* row_scales;    // null: 1
+  const float* col_scales;    // null: 1
+  int64_t stride_col_scales;  // elements between groups
+};
+
 // Compile-time description of one instantiated kernel.
 struct KernelDesc {
   const char* name;   // e.g. "bf16_nn_256x256_w8_m32"
@@ -256,6 +317,15 @@ GroupKernel group_f16(int over_k, int tb, int tile);
 GroupKernel group_fp8(int over_k, int tb, int tile);
 GroupKernel group_f32(int over_k, int tb, int tile);
 const void* act_grad_kernel(int dt);  // null: no such type
+const void* scatter_kernel(int dt, int mode);  // mode 0: copies (dt names the size), 1: weighted, 2: with weight_grad
+const void* combine_kernel(int dt);
+const void* route_count_kernel();
+const void* route_slots_kernel(bool few);  // few: at most kRouteFew experts
+const void* quantize_kernel(int dt);
+// By the type of C; tiles as GroupKernel's, few: kSkinnyRows rows (null: none).
+GroupKernel integer_bf16(int tb, int tile, bool few);
+GroupKernel integer_f16(int tb, int tile, bool few);
+GroupKernel integer_f32(int tb, int tile, bool few);
 const void* bias_sum_kernel(bool many);
 const void* group_sum_kernel(bool many);
 int kernels_d_bf16(const KernelDesc** out);

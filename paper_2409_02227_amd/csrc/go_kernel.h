@@ -22,6 +22,7 @@
 namespace gdy {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
@@ -33,11 +34,18 @@ template <> struct ElemSize<DT_BF16> { static constexpr int v = 2; };
 template <> struct ElemSize<DT_F16> { static constexpr int v = 2; };
 template <> struct ElemSize<DT_FP8> { static constexpr int v = 1; };
 template <> struct ElemSize<DT_F32> { static constexpr int v = 4; };
+template <> struct ElemSize<DT_I8_F16> { static constexpr int v = 1; };
+template <> struct ElemSize<DT_I8_BF16> { static constexpr int v = 1; };
+template <> struct ElemSize<DT_I8_F32> { static constexpr int v = 1; };
+// Products of 8-bit integers: their sums are 32-bit integers, kept as the bits of the
+// accumulators' floats until the epilogue.
+template <int DT> struct IsInt8 { static constexpr bool v = DT >= DT_I8_F16 && DT <= DT_I8_F32; };
 
 // Bytes of one output element: fp32 inputs give fp32 results, the others
 // round to a 16-bit type.
 template <int DT> struct OutSize { static constexpr int v = 2; };
 template <> struct OutSize<DT_F32> { static constexpr int v = 4; };
+template <> struct OutSize<DT_I8_F32> { static constexpr int v = 4; };
 
 // ---------------------------------------------------------------------------
 // MFMA wrappers.  An operand is one lane's fragment (lds_copy.h: FragT); Acc is
@@ -48,6 +56,8 @@ template <> struct OutSize<DT_F32> { static constexpr int v = 4; };
 // assignment, so any consistent lane->K mapping is a valid sum.
 // ---------------------------------------------------------------------------
 template <int DT, int MM> struct Mma;
+// MFMAs that a pair of fragments takes (Mma::part).
+template <int DT> struct MmaParts { static constexpr int v = IsInt8<DT>::v ? 2 : 1; };
 
 template <> struct Mma<DT_BF16, 16> {
   typedef f32x4 Acc;
@@ -74,6 +84,21 @@ template <> struct Mma<DT_FP8, 16> {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 127, 0, 127);
   }
 };
+
+// 8-bit integers: 16 bytes of K per lane and MFMA, so a fragment's 32 bytes take two.
+struct MmaInt8 {
+  typedef f32x4 Acc;  // the bits of four 32-bit integers
+  static constexpr int NACC = 4;
+  template <int PART> static __device__ __forceinline__ Acc part(i32x8 a, i32x8 b, Acc c) {
+    const i32x4 x = {a[4 * PART], a[4 * PART + 1], a[4 * PART + 2], a[4 * PART + 3]};
+    const i32x4 y = {b[4 * PART], b[4 * PART + 1], b[4 * PART + 2], b[4 * PART + 3]};
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y, __builtin_bit_cast(i32x4, c), 0, 0, 0));
+  }
+  static __device__ __forceinline__ Acc run(i32x8 a, i32x8 b, Acc c) { return part<1>(a, b, part<0>(a, b, c)); }
+};
+template <> struct Mma<DT_I8_F16, 16> : MmaInt8 {};
+template <> struct Mma<DT_I8_BF16, 16> : MmaInt8 {};
+template <> struct Mma<DT_I8_F32, 16> : MmaInt8 {};
 
 // fp32: one element of K per lane.
 template <> struct Mma<DT_F32, 16> {

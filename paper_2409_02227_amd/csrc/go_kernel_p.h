@@ -195,12 +195,26 @@ __device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds
       barrier_nowait();
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int ks = 0; ks < C::NKS; ++ks)
+      for (int ks = 0; ks < C::NKS; ++ks) {
+        if constexpr (IsInt8<DT>::v) {  // eight MFMAs between two of one accumulator
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            acc[ha][hb][j][i] = M::run(bf[hb][ks][j], af[ks][i], acc[ha][hb][j][i]);
+            for (int i = 0; i < 4; ++i)
+              acc[ha][hb][j][i] = M::template part<0>(bf[hb][ks][j], af[ks][i], acc[ha][hb][j][i]);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              acc[ha][hb][j][i] = M::template part<1>(bf[hb][ks][j], af[ks][i], acc[ha][hb][j][i]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              acc[ha][hb][j][i] = M::run(bf[hb][ks][j], af[ks][i], acc[ha][hb][j][i]);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
       barrier_nowait();
       __builtin_amdgcn_sched_barrier(0);
@@ -285,19 +299,24 @@ __device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds
       static_assert(8 * Epi::BYTES + 2 * Epi::RP * 256 * 4 <= kPLds, "blocks and sums fit in the ring");
       const EpiOut o = ep(item, tm);
       if (EP::linear && o.linear()) {  // as the plain launch, with a bias
+        float rs[2][4];
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          rs[x >> 2][x & 3] = row_scale<DT>(o, m0 + (x >> 2) * 128 + wm * 64 + (x & 3) * 16 + (lane & 15));
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const int col = hb * 128 + wn * 32 + j * 16 + 4 * (lane >> 4);
-            const f32x4 b = load_bias4<DT>(o, n0 + col);
+            const f32x4 b = load_bias4<DT>(o, n0 + col), cs = load_scales4<DT>(o, n0 + col);
 #pragma unroll
             for (int ha = 0; ha < 2; ++ha) {
               if (ha && half) break;
 #pragma unroll
               for (int i = 0; i < 4; ++i)
                 *(__attribute__((address_space(3))) u32x2*)(smem + (ha * 128 + wm * 64 + i * 16 + (lane & 15)) * kPOutRow +
-                                                            col * 2) = linear4<DT>(acc[ha][hb][j][i], o.scale, b);
+                                                            col * 2) =
+                    linear4<DT>(acc[ha][hb][j][i], o.scale, b, rs[ha][i], cs);
             }
           }
         __syncthreads();

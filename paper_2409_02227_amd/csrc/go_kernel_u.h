@@ -254,12 +254,14 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
       };
       auto mma = [&](const Frag (&af)[C::FM], const Frag (&bf)[C::FN]) {
 #pragma unroll
-        for (int s = 0; s < (C::ES == 4 ? 4 : 1); ++s)  // fp32: the four MFMAs of a K step
+        for (int s = 0; s < (C::ES == 4 ? 4 : MmaParts<DT>::v); ++s)  // fp32: the four MFMAs of a K step
 #pragma unroll
           for (int j = 0; j < C::FN; ++j)
 #pragma unroll
             for (int i = 0; i < C::FM; ++i) {
-              if constexpr (C::ES == 4) {
+              if constexpr (IsInt8<DT>::v) {
+                acc[j][i] = s == 0 ? M::template part<0>(bf[j], af[i], acc[j][i]) : M::template part<1>(bf[j], af[i], acc[j][i]);
+              } else if constexpr (C::ES == 4) {
                 const unsigned b = bf[j][s], a = af[i][s];  // copies: a bit cast of a vector's element takes its first
                 acc[j][i] = M::run(__builtin_bit_cast(float, b), __builtin_bit_cast(float, a), acc[j][i]);
               } else {
@@ -471,10 +473,11 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
 #pragma unroll
         for (int j = 0; j < C::FN; ++j) {
           const int col = wn * WTN + j * 16 + 4 * (lane >> 4);
-          const f32x4 b = load_bias4<DT>(o, n0 + col);
+          const f32x4 b = load_bias4<DT>(o, n0 + col), cs = load_scales4<DT>(o, n0 + col);
 #pragma unroll
           for (int i = 0; i < C::FM; ++i) {
             const int row = wm * WTM + i * 16 + (lane & 15);
+            const float rs = row_scale<DT>(o, m0 + row);
             if constexpr (C::ES == 4) {
               if (m0 + row >= Mrows) continue;
               const f32x4 x = linear_sums<DT>(acc[j][i], o.scale, b);
@@ -488,7 +491,7 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
               }
             } else {
               *(__attribute__((address_space(3))) u32x2*)(smem + row * C::PITCH + col * 2) =
-                  linear4<DT>(acc[j][i], o.scale, b);
+                  linear4<DT>(acc[j][i], o.scale, b, rs, cs);
             }
           }
         }

@@ -149,14 +149,14 @@ __device__ __forceinline__ KArgs tile_args(const KGroup& g, const uint8_t* a, co
 // the cost model of their tiles is fitted to that loop.
 template <int DT, int TA, int TB> struct TileP {
   static constexpr int BM = 256, BN = 256, NT = 512, LDS = kPLds;
-  static __device__ __forceinline__ void run(const KArgs& p, lds_u8* smem, const GroupEpi& e) {
-    p_tiles<DT, TA, TB, true, GroupEpi>(p, 0, 1, smem, e);
+  template <class E> static __device__ __forceinline__ void run(const KArgs& p, lds_u8* smem, const E& e) {
+    p_tiles<DT, TA, TB, true, E>(p, 0, 1, smem, e);
   }
 };
 template <int DT, int TA, int TB, int BM_, int BN_, int WM, int WN, int STAGES> struct TileU {
   static constexpr int BM = BM_, BN = BN_, NT = WM * WN * 64, LDS = UCfg<DT, BM, BN, WM, WN, STAGES>::LDS;
-  static __device__ __forceinline__ void run(const KArgs& p, lds_u8* smem, const GroupEpi& e) {
-    u_tiles<DT, TA, TB, BM, BN, WM, WN, STAGES, true, false, true, GroupEpi>(p, 0, 1, smem, e);
+  template <class E> static __device__ __forceinline__ void run(const KArgs& p, lds_u8* smem, const E& e) {
+    u_tiles<DT, TA, TB, BM, BN, WM, WN, STAGES, true, false, true, E>(p, 0, 1, smem, e);
   }
 };
 

@@ -156,11 +156,17 @@ template <int DT, int TB> struct Skinny {
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          lo += *(const lds_f32x4*)(at + w * (BM * PITCH));
-          hi += *(const lds_f32x4*)(at + w * (BM * PITCH) + 16);
+          const f32x4 l = *(const lds_f32x4*)(at + w * (BM * PITCH)), h = *(const lds_f32x4*)(at + w * (BM * PITCH) + 16);
+          if constexpr (IsInt8<DT>::v) {
+            lo = __builtin_bit_cast(f32x4, __builtin_bit_cast(i32x4, lo) + __builtin_bit_cast(i32x4, l));
+            hi = __builtin_bit_cast(f32x4, __builtin_bit_cast(i32x4, hi) + __builtin_bit_cast(i32x4, h));
+          } else {
+            lo += l;
+            hi += h;
+          }
         }
         float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        x.finish(true, row, v, res, aux);
+        x.finish(true, row, v, res, aux, row_scale<DT>(x.o, row));
       }
       if (part) x.put_sums(smem + TABLE, row, BN, (tid % Epi::LPR) * 8);
     }

@@ -29,6 +29,8 @@ ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4  # gdy_act
 ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
 OVER_ROWS, OVER_K = 0, 1  # gdy_over
 MAX_GROUPS = 4096
+MAX_TOP_K = 64
+ROUTE_ALONE = 4096
 MODES = {"sequential": SEQUENTIAL, "default": DEFAULT, "go": GO,
          "selector": SELECTOR, "forced": FORCED, "forced_grouped": FORCED_GROUPED,
          "cu_partition": CU_PARTITION, "cu_partition_go": CU_PARTITION_GO,
@@ -41,7 +43,8 @@ STATUS = {0: "GDY_OK", 1: "GDY_ERR_INVALID_ARG", 2: "GDY_ERR_UNSUPPORTED", 3: "G
 
 EXPORTS = ("gdy_create", "gdy_destroy", "gdy_set_rc", "gdy_plan", "gdy_execute", "gdy_execute_static",
            "gdy_execute_epilogue", "gdy_execute_epilogue_static", "gdy_execute_grouped", "gdy_grouped_tile",
-           "gdy_execute_act_grad",
+           "gdy_execute_act_grad", "gdy_execute_route", "gdy_execute_scatter", "gdy_execute_combine",
+           "gdy_execute_quantize", "gdy_execute_integer",
            "gdy_set_timing", "gdy_last_kernel_times", "gdy_kernel_times", "gdy_features", "gdy_dispatch_map",
            "gdy_variant_count",
            "gdy_variant_info", "gdy_variant_find", "gdy_isolated_variant",
@@ -89,6 +92,47 @@ class ActGradDesc(ctypes.Structure):
                 ("dy", ctypes.c_void_p), ("lddy", ctypes.c_int64), ("z", ctypes.c_void_p), ("ldz", ctypes.c_int64),
                 ("dz", ctypes.c_void_p), ("lddz", ctypes.c_int64),
                 ("bias_grad", ctypes.c_void_p), ("stride_bias_grad", ctypes.c_int64)]
+
+
+class RouteDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("top_k", ctypes.c_int32), ("experts", ctypes.c_int32),
+                ("ids", ctypes.c_void_p), ("ld_ids", ctypes.c_int64),
+                ("id_bytes", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("slots", ctypes.c_void_p), ("offsets", ctypes.c_void_p)]
+
+
+class ScatterDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("rows", ctypes.c_int64), ("n", ctypes.c_int64),
+                ("top_k", ctypes.c_int32), ("type", ctypes.c_int32), ("slots", ctypes.c_void_p),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("weights", ctypes.c_void_p),
+                ("weights_type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("out", ctypes.c_void_p), ("ldo", ctypes.c_int64), ("z", ctypes.c_void_p), ("ldz", ctypes.c_int64),
+                ("weight_grad", ctypes.c_void_p)]
+
+
+class CombineDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("rows", ctypes.c_int64), ("n", ctypes.c_int64),
+                ("top_k", ctypes.c_int32), ("type", ctypes.c_int32), ("slots", ctypes.c_void_p),
+                ("z", ctypes.c_void_p), ("ldz", ctypes.c_int64), ("weights", ctypes.c_void_p),
+                ("weights_type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64), ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64)]
+
+
+class QuantizeDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("n", ctypes.c_int64), ("type", ctypes.c_int32), ("top_k", ctypes.c_int32),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("slots", ctypes.c_void_p),
+                ("out_rows", ctypes.c_int64), ("q", ctypes.c_void_p), ("ldq", ctypes.c_int64),
+                ("scales", ctypes.c_void_p)]
+
+
+class IntegerDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64),
+                ("c_type", ctypes.c_int32), ("trans_b", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("reserved", ctypes.c_int32), ("offsets", ctypes.c_void_p),
+                ("a", ctypes.c_void_p), ("lda", ctypes.c_int64),
+                ("b", ctypes.c_void_p), ("ldb", ctypes.c_int64), ("stride_b", ctypes.c_int64),
+                ("row_scales", ctypes.c_void_p), ("col_scales", ctypes.c_void_p),
+                ("stride_col_scales", ctypes.c_int64), ("c", ctypes.c_void_p), ("ldc", ctypes.c_int64)]
 
 
 class Plan(ctypes.Structure):
@@ -159,6 +203,11 @@ def load_library(path: str = None) -> ctypes.CDLL:
         "gdy_execute_grouped": (i32, [P, ctypes.POINTER(GroupedDesc), ctypes.POINTER(EpilogueDesc), P]),
         "gdy_grouped_tile": (i32, [P, ctypes.POINTER(GroupedDesc), ctypes.POINTER(i32), ctypes.POINTER(i32)]),
         "gdy_execute_act_grad": (i32, [P, ctypes.POINTER(ActGradDesc), P]),
+        "gdy_execute_route": (i32, [P, ctypes.POINTER(RouteDesc), P]),
+        "gdy_execute_scatter": (i32, [P, ctypes.POINTER(ScatterDesc), P]),
+        "gdy_execute_combine": (i32, [P, ctypes.POINTER(CombineDesc), P]),
+        "gdy_execute_quantize": (i32, [P, ctypes.POINTER(QuantizeDesc), P]),
+        "gdy_execute_integer": (i32, [P, ctypes.POINTER(IntegerDesc), ctypes.POINTER(EpilogueDesc), P]),
         "gdy_set_timing": (i32, [P, i32]),
         "gdy_last_kernel_times": (i32, [P, ctypes.POINTER(ctypes.c_float),
                                         ctypes.POINTER(ctypes.c_float), i32]),
@@ -442,6 +491,217 @@ class ActGrad:
         return d
 
 
+def _matrix(t, name, dtype=None, cols=None):
+    """(rows, columns, leading dimension) of a 2-D tensor."""
+    if t.dim() != 2 or (cols is not None and t.shape[1] != cols) or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be 2-D" + (f" with {cols} columns" if cols is not None else "") +
+                         (f" of {dtype}" if dtype is not None else ""))
+    return t.shape[0], t.shape[1], _rows_of(t, name)
+
+
+def _row_dtype(t, name) -> int:
+    """The code of a floating type; uint8 is not taken for fp8 here."""
+    import torch
+    codes = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32, torch.float8_e4m3fn: FP8_E4M3}
+    if t.dtype not in codes:
+        raise ValueError(f"{name} of {t.dtype}")
+    return codes[t.dtype]
+
+
+def _check_slots(slots, tokens):
+    import torch
+    if slots.dtype != torch.int32 or slots.dim() != 2 or slots.shape[0] != tokens or not slots.is_contiguous():
+        raise ValueError(f"slots must be a contiguous int32 matrix of {tokens} rows")
+    return slots.shape[1]
+
+
+def _pair_weights(d, weights, slots, like):
+    """The fields of the weights of pairs: fp32 or of the rows' type."""
+    import torch
+    if weights is None:
+        return
+    if tuple(weights.shape) != tuple(slots.shape) or not weights.is_contiguous() or \
+            weights.dtype not in (torch.float32, like.dtype):
+        raise ValueError("weights must be contiguous, of the slots' shape, fp32 or of the rows' type")
+    d.weights, d.weights_type = weights.data_ptr(), _row_dtype(weights, "weights")
+
+
+@dataclass
+class Route:
+    """The rows of each expert (gdy_route): from ids (tokens x top_k, int32 or int64, on the
+    device; outside 0 .. experts - 1: none) the slots of the pairs (tokens x top_k, int32)
+    and the bounds of the experts' rows, offsets (experts + 1, int32)."""
+    ids: object
+    slots: object
+    offsets: object
+
+    def tensors(self):
+        return self.ids, self.slots, self.offsets
+
+    def desc(self) -> RouteDesc:
+        import torch
+        d = RouteDesc()
+        if self.ids.dtype not in (torch.int32, torch.int64):
+            raise ValueError("ids must be int32 or int64")
+        d.tokens, d.top_k, d.ld_ids = _matrix(self.ids, "ids")
+        if _check_slots(self.slots, d.tokens) != d.top_k:
+            raise ValueError("slots must have the ids' shape")
+        d.experts = _check_offsets(self.offsets)
+        d.id_bytes = self.ids.element_size()
+        d.ids, d.slots, d.offsets = self.ids.data_ptr(), self.slots.data_ptr(), self.offsets.data_ptr()
+        return d
+
+
+@dataclass
+class Scatter:
+    """Rows to the experts (gdy_scatter): out[slots[t, j]] = weights[t, j] * x[t] (weights None: x[t] itself).
+    weight_grad (fp32, of the slots' shape): the sums of x[t] * z[slots[t, j]], z of out's shape; with x
+    the gradient of a Combine's y, out and weight_grad are those of its z and weights."""
+    x: object
+    slots: object
+    out: object
+    weights: object = None
+    z: object = None
+    weight_grad: object = None
+
+    def tensors(self):
+        return self.x, self.slots, self.out, self.weights, self.z, self.weight_grad
+
+    def desc(self) -> ScatterDesc:
+        import torch
+        d = ScatterDesc()
+        d.type = _row_dtype(self.x, "x")
+        d.tokens, d.n, d.ldx = _matrix(self.x, "x")
+        d.rows, _, d.ldo = _matrix(self.out, "out", self.x.dtype, d.n)
+        d.top_k = _check_slots(self.slots, d.tokens)
+        d.slots, d.x, d.out = self.slots.data_ptr(), self.x.data_ptr(), self.out.data_ptr()
+        _pair_weights(d, self.weights, self.slots, self.x)
+        if (self.weight_grad is None) != (self.z is None) or (self.z is not None and self.weights is None):
+            raise ValueError("z and weight_grad belong together, and need weights")
+        if self.z is not None:
+            if _matrix(self.z, "z", self.x.dtype, d.n)[0] != d.rows:
+                raise ValueError("z must have out's shape")
+            d.z, d.ldz = self.z.data_ptr(), _rows_of(self.z, "z")
+            g = self.weight_grad
+            if g.dtype != torch.float32 or tuple(g.shape) != tuple(self.slots.shape) or not g.is_contiguous():
+                raise ValueError("weight_grad must be contiguous fp32 of the slots' shape")
+            d.weight_grad = g.data_ptr()
+        return d
+
+
+@dataclass
+class Combine:
+    """Rows back from the experts (gdy_combine): y[t] = sum over j of weights[t, j] * z[slots[t, j]], plus residual[t].
+    weights None: their sum, the gradient of a Scatter's x.  residual may be y."""
+    z: object
+    slots: object
+    y: object
+    weights: object = None
+    residual: object = None
+
+    def tensors(self):
+        return self.z, self.slots, self.y, self.weights, self.residual
+
+    def desc(self) -> CombineDesc:
+        d = CombineDesc()
+        d.type = _row_dtype(self.y, "y")
+        d.tokens, d.n, d.ldy = _matrix(self.y, "y")
+        d.rows, _, d.ldz = _matrix(self.z, "z", self.y.dtype, d.n)
+        d.top_k = _check_slots(self.slots, d.tokens)
+        d.slots, d.z, d.y = self.slots.data_ptr(), self.z.data_ptr(), self.y.data_ptr()
+        _pair_weights(d, self.weights, self.slots, self.y)
+        if self.residual is not None:
+            if _matrix(self.residual, "residual", self.y.dtype, d.n)[0] != d.tokens:
+                raise ValueError("residual must have y's shape")
+            d.residual, d.ldr = self.residual.data_ptr(), _rows_of(self.residual, "residual")
+        return d
+
+
+@dataclass
+class Quantize:
+    """Rows in 8-bit integers (gdy_quantize): scales[i] = max |x[i]| / 127 (fp32), q[i] = x[i] / scales[i] to the
+    nearest integer (int8).  slots (rows x top_k): row i goes to the rows slots[i] of q and scales."""
+    x: object
+    q: object
+    scales: object
+    slots: object = None
+
+    def tensors(self):
+        return self.x, self.q, self.scales, self.slots
+
+    def desc(self) -> QuantizeDesc:
+        import torch
+        d = QuantizeDesc()
+        d.type = _row_dtype(self.x, "x")
+        d.rows, d.n, d.ldx = _matrix(self.x, "x")
+        out_rows, _, d.ldq = _matrix(self.q, "q", torch.int8, d.n)
+        if self.scales.dtype != torch.float32 or tuple(self.scales.shape) != (out_rows,) or \
+                not self.scales.is_contiguous():
+            raise ValueError("scales must hold one fp32 value a row of q")
+        if self.slots is not None:
+            top_k = _check_slots(self.slots, d.rows)
+            if d.rows:  # without rows there are no slots either, and their address is null
+                d.top_k, d.out_rows, d.slots = top_k, out_rows, self.slots.data_ptr()
+        elif out_rows != d.rows:
+            raise ValueError("q must have x's shape")
+        d.x, d.q, d.scales = self.x.data_ptr(), self.q.data_ptr(), self.scales.data_ptr()
+        return d
+
+
+@dataclass
+class Int8:
+    """A product of 8-bit integers (gdy_integer): c = act(row_scales[i] * col_scales[j] * (a op(b))[i, j] + bias) +
+    residual, a (rows x K) and b (K x N, or N x K with trans_b) int8, the sums exact, c bf16, fp16 or fp32.
+    row_scales (rows) and col_scales (N): fp32, None: 1.  With offsets (int32, groups + 1) a product
+    grouped by expert over rows, as Grouped: b is 3-D, col_scales and bias N or groups x N."""
+    a: object
+    b: object
+    c: object
+    row_scales: object = None
+    col_scales: object = None
+    offsets: object = None
+    trans_b: int = 0
+    epilogue: object = None
+
+    def tensors(self):
+        return (self.a, self.b, self.c, self.row_scales, self.col_scales, self.offsets) + \
+            (self.epilogue.tensors() if self.epilogue else ())
+
+    def descs(self):
+        """(IntegerDesc, EpilogueDesc or None)."""
+        import torch
+        a, b, c = self.a, self.b, self.c
+        d = IntegerDesc()
+        d.rows, d.k, d.lda = _matrix(a, "a", torch.int8)
+        d.n = c.shape[-1]
+        if _matrix(c, "c")[0] != d.rows:
+            raise ValueError("c must have a's rows")
+        d.ldc, d.c_type = _rows_of(c, "c"), _row_dtype(c, "c")
+        d.trans_b = int(self.trans_b)
+        groups = 0
+        if self.offsets is not None:
+            groups = d.groups = _check_offsets(self.offsets)
+            d.offsets = self.offsets.data_ptr()
+        want = ((groups,) if self.offsets is not None else ()) + ((d.n, d.k) if d.trans_b else (d.k, d.n))
+        if b.dtype != torch.int8 or tuple(b.shape) != want:
+            raise ValueError(f"b must be int8 of shape {want}")
+        if b.dim() == 3:
+            d.ldb, d.stride_b = (_rows_of(b[0], "b") if groups else 1), b.stride(0)
+        else:
+            d.ldb = _rows_of(b, "b")
+        d.a, d.b, d.c = a.data_ptr(), b.data_ptr(), c.data_ptr()
+        for name, t, shapes in (("row_scales", self.row_scales, [(d.rows,)]),
+                                ("col_scales", self.col_scales, [(d.n,)] + ([(groups, d.n)] if groups else []))):
+            if t is None:
+                continue
+            if t.dtype != torch.float32 or tuple(t.shape) not in shapes or (t.shape[-1] > 1 and t.stride(-1) != 1):
+                raise ValueError(f"{name} must be fp32 of shape {' or '.join(map(str, shapes))}, contiguous")
+            setattr(d, name, t.data_ptr())
+            if t.dim() == 2 and groups > 1:
+                d.stride_col_scales = t.stride(0)
+        return d, (None if self.epilogue is None else self.epilogue.desc(c, groups))
+
+
 @dataclass
 class Gemm:
     """One GEMM of a submission, from torch device tensors.
@@ -633,6 +893,52 @@ class Context:
     def execute_act_grad_desc(self, desc, handle):
         """Launch a prepared ActGradDesc."""
         self._check(self.lib.gdy_execute_act_grad(self.h, ctypes.byref(desc), handle))
+
+    def execute_route(self, op: Route, stream=None):
+        """Launch a routing (gdy_execute_route)."""
+        _check_device(self.device, "a routing", *op.tensors())
+        self.execute_route_desc(op.desc(), _stream_handle(stream, self._stream_device()))
+
+    def execute_route_desc(self, desc, handle):
+        """Launch a prepared RouteDesc."""
+        self._check(self.lib.gdy_execute_route(self.h, ctypes.byref(desc), handle))
+
+    def execute_scatter(self, op: Scatter, stream=None):
+        """Launch rows to the experts (gdy_execute_scatter)."""
+        _check_device(self.device, "a scatter", *op.tensors())
+        self.execute_scatter_desc(op.desc(), _stream_handle(stream, self._stream_device()))
+
+    def execute_scatter_desc(self, desc, handle):
+        """Launch a prepared ScatterDesc."""
+        self._check(self.lib.gdy_execute_scatter(self.h, ctypes.byref(desc), handle))
+
+    def execute_combine(self, op: Combine, stream=None):
+        """Launch rows back from the experts (gdy_execute_combine)."""
+        _check_device(self.device, "a combine", *op.tensors())
+        self.execute_combine_desc(op.desc(), _stream_handle(stream, self._stream_device()))
+
+    def execute_combine_desc(self, desc, handle):
+        """Launch a prepared CombineDesc."""
+        self._check(self.lib.gdy_execute_combine(self.h, ctypes.byref(desc), handle))
+
+    def execute_quantize(self, op: Quantize, stream=None):
+        """Launch rows to 8-bit integers (gdy_execute_quantize)."""
+        _check_device(self.device, "a quantisation", *op.tensors())
+        self.execute_quantize_desc(op.desc(), _stream_handle(stream, self._stream_device()))
+
+    def execute_quantize_desc(self, desc, handle):
+        """Launch a prepared QuantizeDesc."""
+        self._check(self.lib.gdy_execute_quantize(self.h, ctypes.byref(desc), handle))
+
+    def execute_int8(self, product: Int8, stream=None):
+        """Launch a product of 8-bit integers (gdy_execute_integer)."""
+        _check_device(self.device, "a product of 8-bit integers", *product.tensors())
+        self.execute_int8_descs(*product.descs(), _stream_handle(stream, self._stream_device()))
+
+    def execute_int8_descs(self, desc, epilogue, handle):
+        """Launch a prepared IntegerDesc (epilogue: an EpilogueDesc or None)."""
+        self._check(self.lib.gdy_execute_integer(self.h, ctypes.byref(desc),
+                                                 None if epilogue is None else ctypes.byref(epilogue), handle))
 
     def set_rc(self, budget_cus: int):
         self._check(self.lib.gdy_set_rc(self.h, budget_cus))
