@@ -470,11 +470,11 @@ gdy_status gdy_execute_act_grad(gdy_ctx* ctx, const gdy_act_grad* op, void* hip_
  *   offsets[e] = the number of pairs of the experts below e (experts + 1 values: the
  *                bounds of gdy_execute_grouped)
  *   slots[t * top_k + j] = the row of the pair, -1 where it has none
- * All of both are written.  More than GDY_ROUTE_ALONE pairs use the context's split-K workspace
+ * All of both are written.  More than GDY_ROUTE_ALONE pairs may use the context's split-K workspace
  * (calls of one context, and replays of graphs captured from them, must be ordered).
  */
 #define GDY_MAX_TOP_K 64
-#define GDY_ROUTE_ALONE 4096
+#define GDY_ROUTE_ALONE 2048
 typedef struct {
   int64_t tokens;                   /* tokens x top_k at most 2^24                          */
   int32_t top_k;                    /* 1 .. GDY_MAX_TOP_K                                   */

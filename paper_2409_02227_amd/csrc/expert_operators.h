@@ -38,10 +38,11 @@ int row_threads_log(int64_t units) {
   return l;
 }
 
-// Workgroups for `rows` rows; kernels loop where 2^22 of them are not enough.
+// Workgroups for `rows` rows; kernels loop where so many are not enough.
+const int kMostRowGrid = 1 << 21;
 unsigned row_grid(int64_t rows, int tpr_log) {
   const int64_t per = kRowThreads >> tpr_log;
-  return (unsigned)std::min<int64_t>((rows + per - 1) / per, 1 << 22);
+  return (unsigned)std::min<int64_t>((rows + per - 1) / per, kMostRowGrid);
 }
 
 hipError_t launch_rows(const void* func, void* args, int64_t rows, int tpr_log, hipStream_t hs) {
@@ -87,23 +88,32 @@ gdy_status launch_route(gdy_ctx* ctx, const gdy_route& g, hipStream_t hs) {
   a.pairs = (int32_t)(g.tokens * g.top_k);
   a.top_k = g.top_k;
   a.experts = g.experts;
-  a.bits = ceil_log2((int64_t)g.experts + 1);
+  a.bits = ceil_log2(g.experts);
   a.wide = g.id_bytes == 8;
   a.dense = g.ld_ids == g.top_k || g.tokens <= 1;
-  const int most_parts = 128;
-  if (a.pairs <= GDY_ROUTE_ALONE) {
-    a.steps = std::max((a.pairs + kRoutePart - 1) / kRoutePart, 1);
-    a.parts = 1;
-  } else {
-    a.steps = std::min((a.pairs + kRoutePart * most_parts - 1) / (kRoutePart * most_parts), kRouteMaxSteps);
-    a.parts = (a.pairs + kRoutePart * a.steps - 1) / (kRoutePart * a.steps);
-    a.counts = (int32_t*)ctx->split_ws;  // at most 261 parts x 4096 experts
-  }
+  a.expert_threads = 1 << std::max(ceil_log2(g.experts), 6);
+  const bool few = g.experts <= kRouteFew;
+  // A step costs a workgroup about 1 us, a second launch 3: 2048 pairs in one part 6.2 us, in two 6.8, 4096 9.2
+  // and 7.1.  2^20 pairs of 64 experts in 256 parts 17.5 us, in 128 24.9, in 1024 31.
+  const bool alone = a.pairs <= GDY_ROUTE_ALONE;
+  const int part = kRoutePart * (alone ? 1 : 256);
+  a.steps = std::max(std::min((a.pairs + part - 1) / part, kRouteMaxSteps), 1);
+  a.parts = std::max((a.pairs + kRoutePart * a.steps - 1) / (kRoutePart * a.steps), 1);
   void* argv[] = {&a};
-  if (a.parts > 1)
-    HIP_TRY(ctx, hipExtLaunchKernel(route_count_kernel(), dim3(a.parts), dim3(kRoutePart), argv, 0, hs, nullptr, nullptr, 0));
-  HIP_TRY(ctx, hipExtLaunchKernel(route_slots_kernel(g.experts <= kRouteFew), dim3(a.parts), dim3(kRoutePart), argv, 0,
-                                  hs, nullptr, nullptr, 0));
+  auto launch = [&](const void* kernel, int grid) {
+    return hipExtLaunchKernel(kernel, dim3(grid), dim3(kRoutePart), argv, 0, hs, nullptr, nullptr, 0);
+  };
+  if (!alone) {
+    a.counts = (int32_t*)ctx->split_ws;  // at most 261 parts x 4096 experts: 4 MiB, and the totals
+    HIP_TRY(ctx, launch(route_count_kernel(few), a.parts));
+    // Every workgroup of the last launch reads the counts, or a launch of its own sums them: 131072 pairs of 128
+    // experts (16384 counts) 9.8 and 10.8 us, of 256 12.2 and 10.9, of 4096 83 and 20.
+    if (a.parts * a.experts > 16384) {
+      a.totals = a.counts + (int64_t)a.parts * a.experts;
+      HIP_TRY(ctx, launch(route_sums_kernel(), (a.experts + 63) / 64));
+    }
+  }
+  HIP_TRY(ctx, launch(route_slots_kernel(few), a.parts));
   return GDY_OK;
 }
 
@@ -256,8 +266,17 @@ gdy_status launch_quantize(gdy_ctx* ctx, const gdy_quantize& g, hipStream_t hs) 
   a.n = (int32_t)g.n;
   a.top_k = g.top_k;
   a.out_rows = (int32_t)g.out_rows;
-  a.tpr_log = row_threads_log((g.n + 15) / 16);
-  HIP_TRY(ctx, launch_rows(quantize_kernel(g.type), &a, g.rows, a.tpr_log, hs));
+  // Rows of more than 4096 elements take 1024 threads where there are few of them ((512, 16384) bf16 12.3 us on 256 and
+  // 10.5 on 1024; (4096, 8192) 28.8, on 512 29.6).
+  const int64_t units = (g.n + 15) / 16;
+  const int threads = units > kRowThreads && units <= 2048 && g.rows <= 4 * ctx->cus ? 1024 : kRowThreads;
+  while ((1 << a.tpr_log) < threads && (1 << a.tpr_log) < units) ++a.tpr_log;
+  const int64_t steps = (units + (1 << a.tpr_log) - 1) >> a.tpr_log;
+  const int64_t per = threads >> a.tpr_log;
+  const int64_t grid = std::min<int64_t>((g.rows + per - 1) / per, kMostRowGrid);
+  void* argv[] = {&a};
+  HIP_TRY(ctx, hipExtLaunchKernel(quantize_kernel(g.type, steps <= 1 ? 1 : steps <= 2 ? 2 : kQuantMost, g.n % 16 == 0),
+                                  dim3((unsigned)grid), dim3(threads), argv, 0, hs, nullptr, nullptr, 0));
   return GDY_OK;
 }
 

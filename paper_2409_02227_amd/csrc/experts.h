@@ -150,95 +150,177 @@ __global__ void __launch_bounds__(kRowThreads) combine_rows(KCombine g) {
 // All counts are integers: no order of additions matters.
 constexpr int kRouteWaves = kRoutePart / 64;
 
-// The expert of pair p (`experts`: none).
+// The expert of pair p (`experts`: none).  Ids are read as dwords; pairs past the last read it.
 __device__ __forceinline__ int pair_expert(const KRoute& g, int p) {
-  if (p >= g.pairs) return g.experts;
-  int64_t at = p;
+  if (g.pairs == 0) return g.experts;  // no last pair to read
+  const int q = min(p, g.pairs - 1);
+  int64_t at = q;
   if (!g.dense) {
-    const int t = p / g.top_k;
-    at = t * g.ld_ids + (p - t * g.top_k);
+    const int t = q / g.top_k;
+    at = t * g.ld_ids + (q - t * g.top_k);
   }
-  const int64_t id = g.wide ? ((const int64_t*)g.ids)[at] : ((const int32_t*)g.ids)[at];
-  return id >= 0 && id < g.experts ? (int)id : g.experts;
+  const int32_t* id = (const int32_t*)g.ids + (at << g.wide);
+  const int lo = id[0], hi = id[g.wide];
+  const bool in = p < g.pairs && (!g.wide || hi == 0) && (unsigned)lo < (unsigned)g.experts;
+  return in ? lo : g.experts;
 }
 
-// The lanes of the wave whose expert is this lane's.
-__device__ __forceinline__ uint64_t same_expert(int e, int bits) {
-  uint64_t m = ~0ull;
-  for (int b = 0; b < bits; ++b) {
-    const bool on = (e >> b) & 1;
-    const uint64_t has = __ballot(on);
-    m &= on ? has : ~has;
+// The lanes of the wave whose expert is this lane's (in: it has one); bits: of the experts' numbers.
+__device__ __forceinline__ uint64_t same_expert(int e, bool in, int bits) {
+  uint64_t m = __ballot(in);
+#pragma unroll 1
+  for (int b0 = 0; b0 < bits; b0 += 4) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const unsigned bit = ((unsigned)e >> b) & 1;
+      const uint64_t has = __ballot(bit);
+      const unsigned off = bit - 1;  // all ones where the bit is 0
+      m &= has ^ ((uint64_t)off << 32 | off);
+    }
+    e >>= 4;
   }
   return m;
 }
 
 // Pairs of each expert in every part: counts[part][expert].
+template <int EXPERTS>
 __global__ void __launch_bounds__(kRoutePart) route_count(KRoute g) {
-  __shared__ int hist[kMaxExperts];
+  __shared__ int hist[EXPERTS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int e = tid; e < g.experts; e += kRoutePart) hist[e] = 0;
+  int p = ((int)blockIdx.x * kRouteWaves + wave) * g.steps * 64 + lane;
+  int e = pair_expert(g, p);
+  for (int i = tid; i < g.experts; i += kRoutePart) hist[i] = 0;
   __syncthreads();
-  const int p0 = ((int)blockIdx.x * kRouteWaves + wave) * g.steps * 64 + lane;
+#pragma unroll 1
   for (int s = 0; s < g.steps; ++s) {
-    const int e = pair_expert(g, p0 + s * 64);
-    const uint64_t m = same_expert(e, g.bits);
+    p += 64;
+    const int next = s + 1 < g.steps ? pair_expert(g, p) : 0;  // a step ahead
+    const uint64_t m = same_expert(e, e < g.experts, g.bits);
     if (e < g.experts && lane == (int)__builtin_ctzll(m)) atomicAdd(&hist[e], (int)__builtin_popcountll(m));
+    e = next;
   }
   __syncthreads();
-  for (int e = tid; e < g.experts; e += kRoutePart) g.counts[(int64_t)blockIdx.x * g.experts + e] = hist[e];
+  for (int i = tid; i < g.experts; i += kRoutePart) g.counts[(int64_t)blockIdx.x * g.experts + i] = hist[i];
+}
+
+// The parts' counts to those of the parts before, and the totals of every expert.  A workgroup has 64
+// experts, a wave consecutive parts.
+__global__ void __launch_bounds__(kRoutePart) route_sums(KRoute g) {
+  __shared__ int sums[kRouteWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = (int)blockIdx.x * 64 + lane;
+  const int per = (g.parts + kRouteWaves - 1) / kRouteWaves, q0 = wave * per, q1 = min(q0 + per, g.parts);
+  int32_t* c = g.counts + e;
+  int x = 0;
+  if (e < g.experts) {
+#pragma unroll 8
+    for (int q = q0; q < q1; ++q) x += c[(int64_t)q * g.experts];
+  }
+  sums[wave][lane] = x;
+  __syncthreads();
+  x = 0;
+  int total = 0;
+  for (int w = 0; w < kRouteWaves; ++w) {
+    if (w < wave) x += sums[w][lane];
+    total += sums[w][lane];
+  }
+  if (e >= g.experts) return;
+  if (wave == 0) g.totals[e] = total;
+#pragma unroll 8
+  for (int q = q0; q < q1; ++q) {
+    const int here = c[(int64_t)q * g.experts];
+    c[(int64_t)q * g.experts] = x;
+    x += here;
+  }
+}
+
+// A wave's LDS accesses are done in the order of its instructions, which this keeps.  (A fence would
+// also wait for the loads of the next step.)
+__device__ __forceinline__ void lds_in_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
 }
 
 // Slots of a part's pairs, and (the first part) the offsets.  parts == 1: this kernel alone.
-// Counts of a wave and expert are 16 bits: a part has fewer than 2^16 pairs.
+// Counts of a wave and expert are 16 bits: a part has fewer than 2^16 pairs.  The only step of
+// a wave is ranked once; several are counted, then read and ranked again.  Without totals (route_sums) the
+// parts' counts are summed by all threads, `wide` experts next to each other.
+// The code is kept short: a call this small waits for its instructions as for its data.
 template <int EXPERTS>
 __global__ void __launch_bounds__(kRoutePart) route_slots(KRoute g) {
   __shared__ int base[EXPERTS];
   __shared__ uint16_t count[kRouteWaves][EXPERTS];
   __shared__ int sums[kRouteWaves];
+  __shared__ int part_total[kRoutePart], part_before[kRoutePart];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int E = g.experts;
-  for (int e = tid; e < E; e += kRoutePart)
-#pragma unroll
-    for (int w = 0; w < kRouteWaves; ++w) count[w][e] = 0;
-  __syncthreads();
   const int p0 = ((int)blockIdx.x * kRouteWaves + wave) * g.steps * 64 + lane;
-  // a step's pairs: their rank among the wave's pairs of their expert, on top of `count`
+  int e = pair_expert(g, p0);
+  for (int i = tid; i < E; i += kRoutePart)
+#pragma unroll
+    for (int w = 0; w < kRouteWaves; ++w) count[w][i] = 0;
+  __syncthreads();
+  // the rank of a step's pair among the wave's pairs of its expert, on top of `count`
   auto rank = [&](int e) {
-    const uint64_t m = same_expert(e, g.bits);
+    const uint64_t m = same_expert(e, e < E, g.bits);
     int r = 0;
     if (e < E) {
       const int before = count[wave][e];  // read by all lanes of the expert, then written by the first
       r = before + (int)__builtin_popcountll(m & ((1ull << lane) - 1));
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+      lds_in_order();
       if (lane == (int)__builtin_ctzll(m)) count[wave][e] = (uint16_t)(before + (int)__builtin_popcountll(m));
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next step's reads
-    __builtin_amdgcn_wave_barrier();
+    lds_in_order();  // before the next step's reads
     return r;
   };
-  for (int s = 0; s < g.steps; ++s) rank(pair_expert(g, p0 + s * 64));
-  __syncthreads();
-  // experts, kRoutePart at a time: counts of the waves before, of the parts before, of the experts before
+  int first_rank = 0;
+  {
+    int at = e;
+#pragma unroll 1
+    for (int s = 0; s < g.steps; ++s) {
+      const int next = s + 1 < g.steps ? pair_expert(g, p0 + (s + 1) * 64) : 0;
+      const int r = rank(at);
+      if (s == 0) first_rank = r;
+      at = next;
+    }
+  }
+  // experts, `wide` at a time: counts of the waves before, of the parts before, of the experts before
+  const int wide = min(kRoutePart, g.expert_threads), rows = kRoutePart / wide;
+  const int column = tid & (wide - 1), row = tid / wide;
   int below = 0;
-  for (int e0 = 0; e0 < E; e0 += kRoutePart) {
-    const int e = e0 + tid;
+#pragma unroll 1
+  for (int e0 = 0; e0 < E; e0 += wide) {
+    const int x = e0 + column;
     int total = 0, before = 0;
-    if (e < E) {
+    if (g.parts > 1) {
+      if (x < E && g.totals) {
+        if (row == 0) before = g.counts[(int64_t)blockIdx.x * E + x], total = g.totals[x];
+      } else if (x < E) {
+        const int32_t* c = g.counts + (int64_t)row * E + x;
+        const int64_t stride = (int64_t)rows * E;
+#pragma unroll 16
+        for (int q = row; q < g.parts; q += rows, c += stride) {
+          before += q < (int)blockIdx.x ? *c : 0;
+          total += *c;
+        }
+      }
+      part_total[tid] = total;
+      part_before[tid] = before;
+    }
+    __syncthreads();  // also behind the waves' counts
+    total = before = 0;
+    const bool mine = row == 0 && x < E;
+    if (mine) {
 #pragma unroll
       for (int w = 0; w < kRouteWaves; ++w) {
-        const int c = count[w][e];
-        count[w][e] = (uint16_t)total;
+        const int c = count[w][x];
+        count[w][x] = (uint16_t)total;
         total += c;
       }
       if (g.parts > 1) {
         total = 0;
-#pragma unroll 8
-        for (int q = 0; q < g.parts; ++q) {
-          const int c = g.counts[(int64_t)q * E + e];
-          before += q < (int)blockIdx.x ? c : 0;
-          total += c;
+        for (int r = 0; r < rows; ++r) {
+          total += part_total[r * wide + tid];
+          before += part_before[r * wide + tid];
         }
       }
     }
@@ -250,17 +332,23 @@ __global__ void __launch_bounds__(kRoutePart) route_slots(KRoute g) {
       if (w < wave) first += sums[w];
       below += sums[w];
     }
-    if (e < E) {
-      base[e] = first + before;
-      if (blockIdx.x == 0) g.offsets[e] = first;
+    if (mine) {
+      base[x] = first + before;
+      if (blockIdx.x == 0) g.offsets[x] = first;
     }
     __syncthreads();
   }
   if (blockIdx.x == 0 && tid == 0) g.offsets[E] = below;
+  if (g.steps == 1) {
+    if (p0 < g.pairs) g.slots[p0] = e < E ? base[e] + count[wave][e] + first_rank : -1;
+    return;
+  }
+#pragma unroll 1
   for (int s = 0; s < g.steps; ++s) {
-    const int p = p0 + s * 64, e = pair_expert(g, p);
+    const int p = p0 + s * 64, next = s + 1 < g.steps ? pair_expert(g, p + 64) : 0;
     const int r = rank(e);
     if (p < g.pairs) g.slots[p] = e < E ? base[e] + r : -1;
+    e = next;
   }
 }
 

@@ -232,12 +232,14 @@ struct KRoute {
   const void* ids;
   int32_t* slots;
   int32_t* offsets;
-  int32_t* counts;         // parts x experts
+  int32_t* counts;         // parts x experts; with totals: of the parts before
+  int32_t* totals;         // one an expert (null: the parts' counts are not summed yet)
   int64_t ld_ids;
   int32_t pairs, top_k, experts;
-  int32_t bits;            // of the numbers 0 .. experts
+  int32_t bits;            // of the experts' numbers
   int32_t wide, dense;     // 64-bit ids; ld_ids == top_k
   int32_t steps, parts;
+  int32_t expert_threads;  // a power of two >= experts, at least 64
 };
 
 // Rows to 8-bit integers (quantize.h).  Pitches are bytes.
@@ -319,9 +321,12 @@ GroupKernel group_f32(int over_k, int tb, int tile);
 const void* act_grad_kernel(int dt);  // null: no such type
 const void* scatter_kernel(int dt, int mode);  // mode 0: copies (dt names the size), 1: weighted, 2: with weight_grad
 const void* combine_kernel(int dt);
-const void* route_count_kernel();
-const void* route_slots_kernel(bool few);  // few: at most kRouteFew experts
-const void* quantize_kernel(int dt);
+const void* route_count_kernel(bool few);  // few: at most kRouteFew experts
+const void* route_sums_kernel();
+const void* route_slots_kernel(bool few);
+// held: steps that a thread keeps (1, 2, or kQuantMost and more); whole: rows of whole steps.
+constexpr int kQuantMost = 4;
+const void* quantize_kernel(int dt, int held, bool whole);
 // By the type of C; tiles as GroupKernel's, few: kSkinnyRows rows (null: none).
 GroupKernel integer_bf16(int tb, int tile, bool few);
 GroupKernel integer_f16(int tb, int tile, bool few);

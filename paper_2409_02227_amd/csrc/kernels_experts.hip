@@ -25,7 +25,10 @@ const void* gdy::combine_kernel(int dt) {
     default: return nullptr;
   }
 }
-const void* gdy::route_count_kernel() { return reinterpret_cast<const void*>(&route_count); }
+const void* gdy::route_count_kernel(bool few) {
+  return few ? reinterpret_cast<const void*>(&route_count<kRouteFew>) : reinterpret_cast<const void*>(&route_count<kMaxExperts>);
+}
+const void* gdy::route_sums_kernel() { return reinterpret_cast<const void*>(&route_sums); }
 const void* gdy::route_slots_kernel(bool few) {
   return few ? reinterpret_cast<const void*>(&route_slots<kRouteFew>) : reinterpret_cast<const void*>(&route_slots<kMaxExperts>);
 }

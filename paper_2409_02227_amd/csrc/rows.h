@@ -5,42 +5,52 @@
 
 namespace gdy {
 
-// Rows may start at any element: loads and stores of 16 bytes need no alignment.
+// Rows may start at any element: loads and stores of several bytes need no alignment.
 typedef u32x4 u32x4_any __attribute__((aligned(1)));
+typedef u32x2 u32x2_any __attribute__((aligned(1)));
+typedef unsigned u32_any __attribute__((aligned(1)));
+typedef uint16_t u16_any __attribute__((aligned(1)));
 
-// VN elements of a row; ES 1 stands for bytes that are copied.
+// The first `bytes` of 16 bytes, by one access for each bit of the number.
+__device__ __forceinline__ u32x4 load_part(const uint8_t* p, int bytes) {
+  u32x4 w = {0u, 0u, 0u, 0u};
+  if (bytes & 8) {
+    const u32x2 x = *(const u32x2_any*)p;
+    w[0] = x[0], w[1] = x[1];
+  }
+  unsigned y = 0;  // the dword that is not whole
+  if (bytes & 4) {
+    const unsigned x = *(const u32_any*)(p + (bytes & 8));
+    w[0] = bytes & 8 ? w[0] : x;
+    w[2] = bytes & 8 ? x : 0u;
+  }
+  if (bytes & 2) y = *(const u16_any*)(p + (bytes & 12));
+  if (bytes & 1) y |= (unsigned)p[bytes & 14] << (8 * (bytes & 2));
+  const int at = bytes >> 2;
+  w[0] = at == 0 ? y : w[0], w[1] = at == 1 ? y : w[1], w[2] = at == 2 ? y : w[2], w[3] = at == 3 ? y : w[3];
+  return w;
+}
+__device__ __forceinline__ void store_part(uint8_t* p, u32x4 w, int bytes) {
+  const int at = bytes >> 2;
+  const unsigned y = at == 0 ? w[0] : at == 1 ? w[1] : at == 2 ? w[2] : w[3];
+  if (bytes & 8) *(u32x2_any*)p = u32x2{w[0], w[1]};
+  if (bytes & 4) *(u32_any*)(p + (bytes & 8)) = bytes & 8 ? w[2] : w[0];
+  if (bytes & 2) *(u16_any*)(p + (bytes & 12)) = (uint16_t)y;
+  if (bytes & 1) p[bytes & 14] = (uint8_t)(y >> (8 * (bytes & 2)));
+}
+
+// 16 bytes of a row, VN elements; ES 1 stands for bytes that are copied.  left: the row's
+// elements from these on.
 template <int DT> struct RowChunk {
   static constexpr int ES = ElemSize<DT>::v, VN = 16 / ES;
   u32x4 w;
   __device__ __forceinline__ void load(const uint8_t* p, int left) {
-    if (left >= VN) {
-      w = *(const u32x4_any*)p;
-    } else {
-      w = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-      for (int e = 0; e < VN; ++e)
-        if (e < left) {
-          unsigned x;
-          if constexpr (ES == 4) x = ((const unsigned*)p)[e];
-          else if constexpr (ES == 2) x = ((const uint16_t*)p)[e];
-          else x = p[e];
-          w[e * ES / 4] |= x << ((e * ES * 8) & 31);
-        }
-    }
+    if (left >= VN) w = *(const u32x4_any*)p;
+    else w = load_part(p, left * ES);
   }
   __device__ __forceinline__ void store(uint8_t* p, int left) const {
-    if (left >= VN) {
-      *(u32x4_any*)p = w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < VN; ++e)
-        if (e < left) {
-          const unsigned x = w[e * ES / 4] >> ((e * ES * 8) & 31);
-          if constexpr (ES == 4) ((unsigned*)p)[e] = x;
-          else if constexpr (ES == 2) ((uint16_t*)p)[e] = (uint16_t)x;
-          else p[e] = (uint8_t)x;
-        }
-    }
+    if (left >= VN) *(u32x4_any*)p = w;
+    else store_part(p, w, left * ES);
   }
   __device__ __forceinline__ float get(int e) const {
     const unsigned x = w[e * ES / 4];

@@ -30,7 +30,7 @@ ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_G
 OVER_ROWS, OVER_K = 0, 1  # gdy_over
 MAX_GROUPS = 4096
 MAX_TOP_K = 64
-ROUTE_ALONE = 4096
+ROUTE_ALONE = 2048
 MODES = {"sequential": SEQUENTIAL, "default": DEFAULT, "go": GO,
          "selector": SELECTOR, "forced": FORCED, "forced_grouped": FORCED_GROUPED,
          "cu_partition": CU_PARTITION, "cu_partition_go": CU_PARTITION_GO,

@@ -63,7 +63,7 @@ def check_route(ctx, ids, experts):
 
 @pytest.mark.parametrize("tokens,top_k,experts", [
     (1, 1, 1), (1, 8, 8), (7, 3, 5), (64, 1, 16), (65, 1, 16), (1024, 1, 255), (1025, 1, 256), (1023, 4, 257), (1024, 4, 64),
-    (1025, 4, 64), (4097, 1, 3), (777, 64, 100), (5000, 2, 4096), (16384, 8, 128), (131073, 1, 60), (40000, 8, 4096),
+    (1025, 4, 64), (4097, 1, 3), (777, 64, 100), (5000, 2, 4096), (16384, 8, 128), (131073, 1, 60), (40000, 8, 4096), (2048, 1, 9), (2049, 1, 9), (16384, 8, 129),
     (0, 2, 16), (33, 2, 0)])
 @pytest.mark.parametrize("wide", [False, True])
 def test_route(ctx, tokens, top_k, experts, wide):
@@ -317,7 +317,8 @@ def check_quantize(ctx, x, pad=0, shift=0, label=""):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("rows,n", [(1, 1), (3, 7), (65, 16), (33, 17), (5, 1024), (300, 1001), (4, 4096), (3, 9000), (2, 20000), (2, 16385)])
+@pytest.mark.parametrize("rows,n", [(1, 1), (3, 7), (65, 16), (33, 17), (5, 1024), (300, 1001), (4, 4096), (3, 9000), (2, 20000), (2, 16385), (3, 16384),
+                                     (1030, 8192), (2100, 4096), (5000, 48), (1, 40000)])
 def test_quantize(ctx, dtype, rows, n):
     gen = torch.Generator().manual_seed(rows + n)
     for pad, shift in ((0, 0), (16, 0), (3, 1)):
