@@ -579,6 +579,9 @@ typedef struct {
 } gdy_integer;
 gdy_status gdy_execute_integer(gdy_ctx* ctx, const gdy_integer* product, const gdy_epilogue* epilogue,
                                void* hip_stream);
+/* The tile of C that a workgroup of gdy_execute_integer computes for this product, as
+ * gdy_grouped_tile tells it. */
+gdy_status gdy_integer_tile(gdy_ctx* ctx, const gdy_integer* product, int32_t* rows, int32_t* cols);
 
 /*
  * Per-kernel timing (Sec. 5.3 measures each GEMM's kernel runtime, with the

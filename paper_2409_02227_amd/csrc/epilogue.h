@@ -287,7 +287,7 @@ template <int DT> __device__ __forceinline__ f32x4 linear_sums(f32x4 x, float sc
   return x;
 }
 template <int DT>
-__device__ __forceinline__ u32x2 linear4(f32x4 x, float scale, f32x4 b, float rs, f32x4 cs) {
+__device__ __forceinline__ u32x2 linear4(f32x4 x, float scale, f32x4 b, float rs = 1.0f, f32x4 cs = f32x4{}) {
   if constexpr (IsInt8<DT>::v) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) x[q] = scaled_int(x[q], rs, cs[q], b[q]);

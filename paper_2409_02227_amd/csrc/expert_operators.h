@@ -344,10 +344,55 @@ gdy_status validate_integer(gdy_ctx* ctx, const gdy_integer& g, const gdy_epilog
   return check_ranges(ctx, ranges);
 }
 
+// What a tile of such a product costs, in us: start + step for each 128 bytes of K where it has a CU to itself, share +
+// share_step where tiles fill the CUs.  Fitted to 244 products of 16 to 4096 rows, N = 1024 to 8192, K = 512 to 8192 and 1,
+// 8 and 32 groups (any: 132 of odd sizes), silu and a bias: their choices take 1.8% (any: 1.6%) more than the fastest
+// tile of each on average, 28% (21%) at most; the fp8 products' rule took 7% and 38%.
+struct IntegerTileCost {
+  int tile, bm, bn;
+  bool copies;  // both operands take copies
+  double start, step, share, share_step;  // share 0: a CU holds one at a time
+};
+const IntegerTileCost kIntegerTiles[] = {
+    {INT_256, 256, 256, true, 13.36, 1.169, 0, 0},          {INT_256, 128, 256, true, 8.81, 0.776, 0, 0},
+    {INT_64x128, 64, 128, true, 5.85, 0.430, 3.63, 0.319},  {INT_64, 64, 64, true, 4.91, 0.303, 2.56, 0.219},
+    {INT_32x64, 32, 64, true, 4.72, 0.230, 1.43, 0.163},    {INT_FEW, 16, 16, true, 4.98, 0.096, 1.65, 0.096},
+    {INT_ANY_128, 128, 128, false, 8.89, 1.161, 7.74, 0.810}, {INT_ANY_64x128, 64, 128, false, 6.87, 0.797, 5.46, 0.587},
+    {INT_ANY_32x128, 32, 128, false, 5.63, 0.601, 3.95, 0.452}, {INT_ANY_32x64, 32, 64, false, 4.91, 0.439, 2.63, 0.325}};
+
+// Groups' sizes are unknown here: their row tiles as group_rows_tile counts them.
+const IntegerTileCost& integer_tile_of(const gdy_ctx* ctx, const gdy_integer& g, bool copies) {
+  const double cus = ctx->cus, groups = g.offsets ? (double)std::min<int64_t>(g.groups, g.rows) : 1.0;
+  const double avg = (double)g.rows / groups, steps = std::ceil((double)g.k / 128);
+  const IntegerTileCost* best = nullptr;
+  double best_t = 0;
+  for (const IntegerTileCost& c : kIntegerTiles) {
+    if (c.copies != copies || (c.tile == INT_FEW && !g.trans_b)) continue;
+    const double rows = groups <= 1 ? std::ceil((double)g.rows / c.bm) : groups / (1.0 - std::exp(-c.bm / avg));
+    const double n = rows * (double)((g.n + c.bn - 1) / c.bn) / cus, alone = c.start + c.step * steps;
+    double t;
+    if (c.share > 0) {
+      t = std::max(alone, std::ceil(n - 0.01) * (c.share + c.share_step * steps));
+    } else {  // a last wave of up to half the CUs runs as halves of 256-row tiles
+      const double full = std::floor(n), rest = n - full;
+      t = alone * (full + (rest == 0 ? 0.0 : c.bm == 256 && rest <= 0.5 ? 0.65 : 1.0));
+    }
+    if (!best || t < best_t) best = &c, best_t = t;
+  }
+  return *best;
+}
+
+// Whether a valid product computes a tile at all, and which.
+bool integer_has_tiles(const gdy_integer& g) { return (!g.offsets || g.groups > 0) && g.rows > 0 && g.n > 0; }
+bool integer_a_copies(const gdy_integer& g) { return copies_ok(g.a, g.lda, g.k, 1, true, 0); }
+bool integer_b_copies(const gdy_integer& g) {
+  return copies_ok(g.b, g.ldb, g.k, 1, g.trans_b != 0, g.offsets && g.groups > 1 ? g.stride_b : 0);
+}
+
 gdy_status launch_integer(gdy_ctx* ctx, const gdy_integer& g, const gdy_epilogue* ep, hipStream_t hs) {
+  if (!integer_has_tiles(g)) return GDY_OK;
   const bool grouped = g.offsets != nullptr;
   const int groups = grouped ? g.groups : 1;
-  if (groups == 0 || g.rows == 0 || g.n == 0) return GDY_OK;
   const int os = g.c_type == GDY_F32 ? 4 : 2;
   const bool many = groups > 1;
   KInteger q;
@@ -371,8 +416,8 @@ gdy_status launch_integer(gdy_ctx* ctx, const gdy_integer& g, const gdy_epilogue
   a.scale = 1.0f;
   auto vec = [&](const void* p, int64_t ld) { return (uintptr_t)p % 8 == 0 && (ld * os) % 8 == 0; };
   a.c_vec = vec(g.c, g.ldc);
-  a.a_dma = copies_ok(g.a, g.lda, g.k, 1, true, 0);
-  a.b_dma = copies_ok(g.b, g.ldb, g.k, 1, g.trans_b != 0, a.stride_b);
+  a.a_dma = integer_a_copies(g);
+  a.b_dma = integer_b_copies(g);
   a.xcd_cus = std::max(ctx->cus / kXcds, 1);
   if (ep) {
     a.epi.bias = (const uint8_t*)ep->bias;
@@ -383,29 +428,11 @@ gdy_status launch_integer(gdy_ctx* ctx, const gdy_integer& g, const gdy_epilogue
     a.epi.res_vec = vec(ep->residual, ep->ldr);
     a.epi.act = ep->act;
   }
-  // the tile of the fp8 product of these sizes
-  gdy_grouped like;
-  std::memset(&like, 0, sizeof like);
-  like.a_type = like.b_type = GDY_FP8_E4M3;
-  like.groups = groups;
-  like.rows = g.rows;
-  like.n = g.n;
-  like.k = g.k;
-  like.trans_b = g.trans_b;
-  const bool copies = a.a_dma && a.b_dma;
-  auto kernel = [&](int tile, bool few) {
-    return g.c_type == GDY_BF16 ? integer_bf16(g.trans_b, tile, few)
-           : g.c_type == GDY_F16 ? integer_f16(g.trans_b, tile, few) : integer_f32(g.trans_b, tile, few);
-  };
-  GroupKernel kern;
-  if (g.trans_b && group_rows_few(like, copies)) {
-    kern = kernel(0, true);
-    a.bm = kern.bm;
-  } else {
-    const GroupTileCost& tile = group_rows_tile(ctx, like, copies);
-    kern = kernel(tile.tile, false);
-    a.bm = tile.bm;
-  }
+  const IntegerTileCost& tile = integer_tile_of(ctx, g, a.a_dma && a.b_dma);
+  const GroupKernel kern = g.c_type == GDY_BF16  ? integer_bf16(g.trans_b, tile.tile)
+                           : g.c_type == GDY_F16 ? integer_f16(g.trans_b, tile.tile)
+                                                 : integer_f32(g.trans_b, tile.tile);
+  a.bm = tile.bm;
   a.max_slots = (int32_t)(grouped ? max_row_tiles(g.rows, groups, a.bm) : (g.rows + a.bm - 1) / a.bm);
   const int64_t tn = (g.n + kern.bn - 1) / kern.bn;
   const int64_t grid = (((int64_t)a.max_slots * tn + kXcds - 1) / kXcds + a.xcd_cus / 2) * kXcds;

@@ -2824,6 +2824,24 @@ gdy_status gdy_execute_integer(gdy_ctx* ctx, const gdy_integer* product, const g
   }
 }
 
+gdy_status gdy_integer_tile(gdy_ctx* ctx, const gdy_integer* product, int32_t* rows, int32_t* cols) {
+  if (!ctx) return GDY_ERR_INVALID_ARG;
+  ctx->err.clear();
+  try {
+    if (!product || !rows || !cols) return fail(ctx, GDY_ERR_INVALID_ARG, "null product, rows or cols");
+    const gdy_status s = validate_integer(ctx, *product, nullptr);
+    if (s != GDY_OK) return s;
+    *rows = *cols = 0;
+    if (!integer_has_tiles(*product)) return GDY_OK;
+    const IntegerTileCost& c = integer_tile_of(ctx, *product, integer_a_copies(*product) && integer_b_copies(*product));
+    *rows = c.bm;
+    *cols = c.bn;
+    return GDY_OK;
+  } catch (...) {
+    return fail(ctx, GDY_ERR_NOMEM, "host allocation failed");
+  }
+}
+
 gdy_status gdy_dispatch_map(gdy_ctx* ctx, const gdy_gemm* gemms, int32_t n, int32_t mode, int32_t forced_cd,
                             int32_t dispatch, int32_t max_workgroups, int32_t* grid, int32_t* gemm_of_wg,
                             int32_t* first_item, int32_t* item_stride, int64_t* items_of_gemm) {

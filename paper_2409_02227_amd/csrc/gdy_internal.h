@@ -327,10 +327,14 @@ const void* route_slots_kernel(bool few);
 // held: steps that a thread keeps (1, 2, or kQuantMost and more); whole: rows of whole steps.
 constexpr int kQuantMost = 4;
 const void* quantize_kernel(int dt, int held, bool whole);
-// By the type of C; tiles as GroupKernel's, few: kSkinnyRows rows (null: none).
-GroupKernel integer_bf16(int tb, int tile, bool few);
-GroupKernel integer_f16(int tb, int tile, bool few);
-GroupKernel integer_f32(int tb, int tile, bool few);
+// Products of 8-bit integers by the type of C (null: no such tile).  For operands that both take copies: 256 x 256
+// tiles (also as 128 rows), smaller ones, and kSkinnyRows rows with B stored N x K; for any operands INT_ANY_*.
+enum : int {
+  INT_256, INT_64x128, INT_64, INT_32x64, INT_FEW, INT_ANY_128, INT_ANY_64x128, INT_ANY_32x128, INT_ANY_32x64
+};
+GroupKernel integer_bf16(int tb, int tile);
+GroupKernel integer_f16(int tb, int tile);
+GroupKernel integer_f32(int tb, int tile);
 const void* bias_sum_kernel(bool many);
 const void* group_sum_kernel(bool many);
 int kernels_d_bf16(const KernelDesc** out);

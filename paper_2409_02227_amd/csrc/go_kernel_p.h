@@ -294,29 +294,26 @@ __device__ __forceinline__ void p_tiles(const KArgs& args, int lwg, int nwg, lds
     // two rows an instruction, where the accumulators' own order gives 32.
     // The 528-byte row pitch keeps a half wave's 16 rows of 16 bytes on
     // distinct banks.
-    if constexpr (EP::on) {  // a wave's quadrants one after another, by columns
+    if constexpr (EP::on && IsInt8<DT>::v) {
+      ep.finish(acc, half, smem);
+    } else if constexpr (EP::on) {  // a wave's quadrants one after another, by columns
       typedef EpiWave<DT, 64, 32, EP::ahead> Epi;
       static_assert(8 * Epi::BYTES + 2 * Epi::RP * 256 * 4 <= kPLds, "blocks and sums fit in the ring");
       const EpiOut o = ep(item, tm);
       if (EP::linear && o.linear()) {  // as the plain launch, with a bias
-        float rs[2][4];
-#pragma unroll
-        for (int x = 0; x < 8; ++x)
-          rs[x >> 2][x & 3] = row_scale<DT>(o, m0 + (x >> 2) * 128 + wm * 64 + (x & 3) * 16 + (lane & 15));
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const int col = hb * 128 + wn * 32 + j * 16 + 4 * (lane >> 4);
-            const f32x4 b = load_bias4<DT>(o, n0 + col), cs = load_scales4<DT>(o, n0 + col);
+            const f32x4 b = load_bias4<DT>(o, n0 + col);
 #pragma unroll
             for (int ha = 0; ha < 2; ++ha) {
               if (ha && half) break;
 #pragma unroll
               for (int i = 0; i < 4; ++i)
                 *(__attribute__((address_space(3))) u32x2*)(smem + (ha * 128 + wm * 64 + i * 16 + (lane & 15)) * kPOutRow +
-                                                            col * 2) =
-                    linear4<DT>(acc[ha][hb][j][i], o.scale, b, rs[ha][i], cs);
+                                                            col * 2) = linear4<DT>(acc[ha][hb][j][i], o.scale, b);
             }
           }
         __syncthreads();

@@ -21,6 +21,143 @@ template <int DT> struct IntegerEpi : GroupEpi {
     o.col_scales = g->col_scales ? g->col_scales + e * g->stride_col_scales + n0 : nullptr;
     return o;
   }
+
+  // The end of a 256 x 256 tile (p_tiles): acc[half of A][half of B][16-column block][16-row block].  The sums pass
+  // through LDS, so that a lane has eight consecutive columns of a row.  All that the arithmetic reads (scales,
+  // bias, the first residual rows) is on its way before the sums are laid down: with loads in front of each group of
+  // rows the end of a tile took 14 us of the 44 that a tile of 8192 rows in 16 groups x 4096, K = 2048, with silu
+  // takes in all, now 10.  Tiles without a residual leave by quadrants (28.5 us for (4096, 8192, 128) with silu, by rows
+  // 30.5), those with one by rows, whose loads and stores are of 256 bytes (45.7 us, by quadrants 49.1).
+  __device__ __forceinline__ void finish(const f32x4 (&acc)[2][2][2][4], bool half, lds_u8* smem) const {
+    const EpiOut o = (*this)(0, 0);
+    if (o.res) by_rows(o, acc, half, smem);
+    else by_quadrants(o, acc, half, smem);
+  }
+
+  // Eight sums of a row to C.
+  static __device__ __forceinline__ void put8(const lds_u8* src, float rs, const f32x4 (&cs)[2], const float (&b)[8], int act,
+                                              const Row8<DT>* res, Rsrc rc, int off, bool vec, int left) {
+    const f32x4 lo = *(const __attribute__((address_space(3))) f32x4*)src;
+    const f32x4 hi = *(const __attribute__((address_space(3))) f32x4*)(src + 16);
+    float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] = scaled_int(x[q], rs, cs[q / 4][q & 3], b[q]);
+    apply_values(x, act);
+    if (res) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] += res->get(q);
+    }
+    Row8<DT> w;
+    w.set(x);
+    w.store(rc, off, vec, left);
+  }
+
+  // 128 columns at a time, 16 lanes a row, a wave 32 rows, four of them a pass.
+  __device__ __forceinline__ void by_rows(const EpiOut& o, const f32x4 (&acc)[2][2][2][4], bool half, lds_u8* smem) const {
+    constexpr int OS = OutSize<DT>::v, PITCH = 128 * 4 + 16, PASSES = 8;
+    constexpr int AHEAD = OS == 4 ? 1 : 4;  // passes with their residuals on the way: as registers allow
+    static_assert(256 * PITCH <= kPLds, "half the columns fit in the ring");
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), wm = wave >> 2, wn = wave & 3;
+    const Rsrc rc = make_rsrc(o.c, o.c_bytes), rr = make_rsrc(o.res, ((o.m - 1) * o.ldr + o.n) * OS);
+    const int r0 = wave * 32 + (lane >> 4), c0 = (lane & 15) * 8;
+    float rs[PASSES], b[2][8];
+    f32x4 cs[2][2];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) rs[p] = row_scale<DT>(o, r0 + 4 * p);
+#pragma unroll
+    for (int hb = 0; hb < 2; ++hb) {
+      cs[hb][0] = load_scales4<DT>(o, hb * 128 + c0), cs[hb][1] = load_scales4<DT>(o, hb * 128 + c0 + 4);
+      load_bias<DT>(o, hb * 128 + c0, b[hb]);
+    }
+    const bool live = wave * 32 < o.m;  // some of the wave's rows lie inside C
+#pragma unroll
+    for (int hb = 0; hb < 2; ++hb) {
+      const int left = o.n - hb * 128 - c0;
+      const bool whole = __ballot(left > 0 && left < 8) == 0;  // every lane has all its columns inside C, or none
+      const bool c_vec = whole && (OS == 4 || o.c_vec), r_vec = whole && (OS == 4 || o.res_vec);
+      auto at = [&](int p, int ld) {
+        return r0 + 4 * p < o.m && left > 0 ? ((r0 + 4 * p) * ld + hb * 128 + c0) * OS : kOutOfRange;
+      };
+      auto inside = [&](int p) { return r0 + 4 * p < o.m ? left : 0; };
+      Row8<DT> res[AHEAD];
+      auto load = [&](int p0) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) res[u].load(rr, at(p0 + u, o.ldr), r_vec, inside(p0 + u));
+      };
+      if (live) load(0);
+      if (hb) __syncthreads();  // the half before is read
+#pragma unroll
+      for (int ha = 0; ha < 2; ++ha) {
+        if (ha && half) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            *(__attribute__((address_space(3))) f32x4*)(smem + (ha * 128 + wm * 64 + i * 16 + (lane & 15)) * PITCH +
+                                                        (wn * 32 + j * 16 + 4 * (lane >> 4)) * 4) = acc[ha][hb][j][i];
+      }
+      __syncthreads();
+      if (!live) continue;
+#pragma unroll
+      for (int p0 = 0; p0 < PASSES; p0 += AHEAD) {
+        if (p0) load(p0);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+          put8(smem + (r0 + 4 * (p0 + u)) * PITCH + c0 * 4, rs[p0 + u], cs[hb], b[hb], o.act, &res[u], rc,
+               at(p0 + u, o.ldc), c_vec, inside(p0 + u));
+      }
+    }
+  }
+
+  // The wave's quadrants of 64 x 32 through LDS of its own, in two places: no wave waits for another.  Four lanes a
+  // row, 16 rows a pass.
+  __device__ __forceinline__ void by_quadrants(const EpiOut& o, const f32x4 (&acc)[2][2][2][4], bool half,
+                                               lds_u8* smem) const {
+    constexpr int OS = OutSize<DT>::v, PITCH = 32 * 4 + 16, BLOCK = 64 * PITCH, PASSES = 4;
+    static_assert(2 * 8 * BLOCK <= kPLds, "two blocks a wave fit in the ring");
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), wm = wave >> 2, wn = wave & 3;
+    const Rsrc rc = make_rsrc(o.c, o.c_bytes);
+    const int r0 = wm * 64 + (lane >> 2), c0 = wn * 32 + (lane & 3) * 8;  // of quadrant 0
+    float rs[2][PASSES], b[2][8];
+    f32x4 cs[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) rs[h][p] = row_scale<DT>(o, r0 + h * 128 + 16 * p);
+      cs[h][0] = load_scales4<DT>(o, c0 + h * 128), cs[h][1] = load_scales4<DT>(o, c0 + h * 128 + 4);
+      load_bias<DT>(o, c0 + h * 128, b[h]);
+    }
+    auto place = [&](int q) { return smem + (q & 1) * (8 * BLOCK) + wave * BLOCK; };
+    // quadrant q: columns q / 2, rows q % 2
+    auto dump = [&](int q) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          *(__attribute__((address_space(3))) f32x4*)(place(q) + (i * 16 + (lane & 15)) * PITCH + (j * 16 + 4 * (lane >> 4)) * 4) =
+              acc[q & 1][q >> 1][j][i];
+    };
+    auto done = [&](int q) { return half && (q & 1); };  // no such rows
+    dump(0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (q < 3 && !done(q + 1)) dump(q + 1);
+      if (done(q)) continue;
+      const int left = o.n - c0 - (q >> 1) * 128;  // columns of C from this lane's on
+      const bool vec = __ballot(left > 0 && left < 8) == 0 && (OS == 4 || o.c_vec);
+      // the wave's own sums, in LDS in the order of its instructions
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        const int row = r0 + (q & 1) * 128 + 16 * p;
+        put8(place(q) + ((lane >> 2) + 16 * p) * PITCH + (lane & 3) * 32, rs[q & 1][p], cs[q >> 1], b[q >> 1], o.act, nullptr,
+             rc, row < o.m && left > 0 ? (row * o.ldc + c0 + (q >> 1) * 128) * OS : kOutOfRange, vec, row < o.m ? left : 0);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next sums in this place
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
 };
 
 // The tile of C that this workgroup computes, in tiles of bm x bn rows; false: none.  halves:
@@ -52,12 +189,13 @@ __device__ __forceinline__ bool integer_tile(const KGroup& g, int bm, int bn, bo
 }
 
 template <int DT, int TB, class T>
-__global__ void __launch_bounds__(T::NT) integer_rows(KInteger q) {
+__global__ void __launch_bounds__(T::NT, T::NT == 512 ? 2 : T::LDS > 80 * 1024 ? 1 : 2) integer_rows(KInteger q) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDS];
   const KGroup& g = q.g;
-  const int bm = T::BM == 256 ? g.bm : T::BM;  // the 256 x 256 kernel has 128-row tiles too
+  constexpr bool P = T::BN == 256;  // the 256 x 256 kernel has 128-row tiles too
+  const int bm = P ? g.bm : T::BM;
   IntegerEpi<DT> e;
-  if (!integer_tile<DT>(g, bm, T::BN, T::BM == 256 && bm == 256, e)) return;
+  if (!integer_tile<DT>(g, bm, T::BN, P && bm == 256, e)) return;
   const uint8_t* a = g.a + (int64_t)e.row * g.lda;
   const uint8_t* b = g.b + e.e * g.stride_b + (TB == 1 ? (int64_t)e.n0 * g.ldb : (int64_t)e.n0);
   T::run(tile_args<DT, 0, TB>(g, a, b, e.m, e.n, g.k), (lds_u8*)smem, e);
@@ -75,23 +213,36 @@ __global__ void __launch_bounds__(512) integer_few(KInteger q) {
           0, (lds_u8*)smem);
 }
 
+// Tiles of go_kernel_u.h for operands that both take copies, with a ring of STAGES and the fragments of a K tile read
+// in front of its MFMAs (TileU's loop takes any operands and reads them step by step: 244 products of 16 to 4096 rows
+// ran 2% slower on its 64 x 128 tiles, (512, 4096, 4096) 21.3 us and 20.3).
+template <int DT, int TB, int BM_, int BN_, int WM, int WN, int STAGES> struct TileD {
+  static constexpr int BM = BM_, BN = BN_, NT = WM * WN * 64, LDS = UCfg<DT, BM, BN, WM, WN, STAGES>::LDS;
+  template <class E> static __device__ __forceinline__ void run(const KArgs& p, lds_u8* smem, const E& e) {
+    u_tiles<DT, 0, TB, BM, BN, WM, WN, STAGES, false, false, true, E>(p, 0, 1, smem, e);
+  }
+};
+
 #define GDY_INTEGER(DT, TB, ...) \
   group_kernel<__VA_ARGS__>(reinterpret_cast<const void*>(&integer_rows<DT, TB, __VA_ARGS__>))
+// The tiles of INT_* (gdy_internal.h).
 template <int DT, int TB> GroupKernel integer_kernel(int tile) {
   switch (tile) {
-    case 0: return GDY_INTEGER(DT, TB, TileP<DT, 0, TB>);
-    case 1: return GDY_INTEGER(DT, TB, TileU<DT, 0, TB, 128, 128, 2, 2, 2>);
-    case 2: return GDY_INTEGER(DT, TB, TileU<DT, 0, TB, 64, 128, 2, 2, 3>);
-    case 3: return GDY_INTEGER(DT, TB, TileU<DT, 0, TB, 32, 128, 1, 4, 4>);
-    case 4: return GDY_INTEGER(DT, TB, TileU<DT, 0, TB, 32, 64, 1, 4, 4>);
+    case INT_256: return GDY_INTEGER(DT, TB, TileP<DT, 0, TB>);
+    case INT_64x128: return GDY_INTEGER(DT, TB, TileD<DT, TB, 64, 128, 2, 2, 3>);
+    case INT_64: return GDY_INTEGER(DT, TB, TileD<DT, TB, 64, 64, 2, 2, 4>);
+    case INT_32x64: return GDY_INTEGER(DT, TB, TileD<DT, TB, 32, 64, 1, 4, 4>);
+    case INT_ANY_128: return GDY_INTEGER(DT, TB, TileU<DT, 0, TB, 128, 128, 2, 2, 2>);
+    case INT_ANY_64x128: return GDY_INTEGER(DT, TB, TileU<DT, 0, TB, 64, 128, 2, 2, 3>);
+    case INT_ANY_32x128: return GDY_INTEGER(DT, TB, TileU<DT, 0, TB, 32, 128, 1, 4, 4>);
+    case INT_ANY_32x64: return GDY_INTEGER(DT, TB, TileU<DT, 0, TB, 32, 64, 1, 4, 4>);
+    case INT_FEW:
+      if constexpr (TB == 1)
+        return GroupKernel{reinterpret_cast<const void*>(&integer_few<DT>), kSkinnyRows, Skinny<DT, 1>::BN, 512};
     default: return GroupKernel{nullptr, 0, 0, 0};
   }
 }
-template <int DT> GroupKernel integer_kernels(int tb, int tile, bool few) {
-  if (few) {
-    if (!tb) return GroupKernel{nullptr, 0, 0, 0};
-    return GroupKernel{reinterpret_cast<const void*>(&integer_few<DT>), kSkinnyRows, Skinny<DT, 1>::BN, 512};
-  }
+template <int DT> GroupKernel integer_kernels(int tb, int tile) {
   return tb ? integer_kernel<DT, 1>(tile) : integer_kernel<DT, 0>(tile);
 }
 

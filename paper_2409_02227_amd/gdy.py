@@ -44,7 +44,7 @@ STATUS = {0: "GDY_OK", 1: "GDY_ERR_INVALID_ARG", 2: "GDY_ERR_UNSUPPORTED", 3: "G
 EXPORTS = ("gdy_create", "gdy_destroy", "gdy_set_rc", "gdy_plan", "gdy_execute", "gdy_execute_static",
            "gdy_execute_epilogue", "gdy_execute_epilogue_static", "gdy_execute_grouped", "gdy_grouped_tile",
            "gdy_execute_act_grad", "gdy_execute_route", "gdy_execute_scatter", "gdy_execute_combine",
-           "gdy_execute_quantize", "gdy_execute_integer",
+           "gdy_execute_quantize", "gdy_execute_integer", "gdy_integer_tile",
            "gdy_set_timing", "gdy_last_kernel_times", "gdy_kernel_times", "gdy_features", "gdy_dispatch_map",
            "gdy_variant_count",
            "gdy_variant_info", "gdy_variant_find", "gdy_isolated_variant",
@@ -208,6 +208,7 @@ def load_library(path: str = None) -> ctypes.CDLL:
         "gdy_execute_combine": (i32, [P, ctypes.POINTER(CombineDesc), P]),
         "gdy_execute_quantize": (i32, [P, ctypes.POINTER(QuantizeDesc), P]),
         "gdy_execute_integer": (i32, [P, ctypes.POINTER(IntegerDesc), ctypes.POINTER(EpilogueDesc), P]),
+        "gdy_integer_tile": (i32, [P, ctypes.POINTER(IntegerDesc), ctypes.POINTER(i32), ctypes.POINTER(i32)]),
         "gdy_set_timing": (i32, [P, i32]),
         "gdy_last_kernel_times": (i32, [P, ctypes.POINTER(ctypes.c_float),
                                         ctypes.POINTER(ctypes.c_float), i32]),
@@ -939,6 +940,13 @@ class Context:
         """Launch a prepared IntegerDesc (epilogue: an EpilogueDesc or None)."""
         self._check(self.lib.gdy_execute_integer(self.h, ctypes.byref(desc),
                                                  None if epilogue is None else ctypes.byref(epilogue), handle))
+
+    def int8_tile(self, product):
+        """(rows, columns) of the tile that an Int8 or IntegerDesc runs on (gdy_integer_tile)."""
+        d = product if isinstance(product, IntegerDesc) else product.descs()[0]
+        rows, cols = ctypes.c_int32(), ctypes.c_int32()
+        self._check(self.lib.gdy_integer_tile(self.h, ctypes.byref(d), ctypes.byref(rows), ctypes.byref(cols)))
+        return rows.value, cols.value
 
     def set_rc(self, budget_cus: int):
         self._check(self.lib.gdy_set_rc(self.h, budget_cus))

@@ -329,3 +329,30 @@ def test_8bit_experts_in_a_graph(ctx):
         assert torch.equal(x.y, want), rep
     del graph
     torch.cuda.synchronize()
+
+
+# products that between them run on all tiles, for operands that take copies and for others
+TILES = [(20, 512, 144), (100, 16390, 144), (200, 8200, 130), (250, 8200, 300), (300, 16390, 144), (200, 16400, 144),
+         (700, 2050, 150), (500, 8208, 144), (20, 16400, 144)]
+
+
+@pytest.mark.parametrize("tb", [0, 1])
+@pytest.mark.parametrize("pad", [16, 3])
+def test_every_tile(ctx, tb, pad):
+    """Each tile dense, in ragged groups, with and without a residual; both sides of a K tile."""
+    found = set()
+    for rows, n, k in TILES:
+        n += (-n) % 16 if pad == 16 else 0
+        k += (-k) % 16 if pad == 16 else 0
+        for offsets in (None, [0, rows // 2 - 3, rows // 2 - 3, rows - 5]):
+            for residual in (False, True):
+                x = Product("bf16", rows, offsets, n, k, tb, "gelu" if residual else "none", "own", residual, pad=pad)
+                run(ctx, x)
+                found.add(ctx.int8_tile(x.product))
+    few = Product("f16", 3, None, 200, 4096, tb, pad=pad)  # B stored N x K
+    run(ctx, few)
+    found.add(ctx.int8_tile(few.product))
+    if pad == 16:
+        assert found == {(256, 256), (128, 256), (64, 128), (64, 64), (32, 64)} | ({(16, 16)} if tb else set()), found
+    else:
+        assert found == {(128, 128), (64, 128), (32, 128), (32, 64)}, found
