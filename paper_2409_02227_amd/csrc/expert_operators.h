@@ -435,7 +435,8 @@ gdy_status launch_integer(gdy_ctx* ctx, const gdy_integer& g, const gdy_epilogue
   a.bm = tile.bm;
   a.max_slots = (int32_t)(grouped ? max_row_tiles(g.rows, groups, a.bm) : (g.rows + a.bm - 1) / a.bm);
   const int64_t tn = (g.n + kern.bn - 1) / kern.bn;
-  const int64_t grid = (((int64_t)a.max_slots * tn + kXcds - 1) / kXcds + a.xcd_cus / 2) * kXcds;
+  const int64_t halves = a.bm == 256 ? a.xcd_cus / 2 : 0;  // workgroups for the last tiles' other halves
+  const int64_t grid = (((int64_t)a.max_slots * tn + kXcds - 1) / kXcds + halves) * kXcds;
   if (grid * kern.threads > UINT32_MAX)  // threads of a launch
     return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: a grid of %lld workgroups", (long long)grid);
   void* argv[] = {&q};

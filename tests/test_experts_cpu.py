@@ -359,3 +359,21 @@ def test_wait_states_and_no_scratch(tmp_path, unit):
 @pytest.mark.parametrize("unit", ["kernels_experts", "kernels_quantize"])
 def test_no_scratch(tmp_path, unit):
     check_code(unit, *device_code(tmp_path, unit))
+
+
+def test_integer_tile(ctx):
+    tile = lambda kw: ctx.int8_tile(filled(gdy.IntegerDesc(), INTEGER, kw))  # noqa: E731
+    big = dict(DENSE, rows=8192, n=8192, k=8192, lda=8192, ldb=8192, ldc=8192, a=1 << 42, b=1 << 43, c=1 << 44)
+    assert tile(big) == (256, 256)
+    assert tile(dict(big, a=(1 << 42) + 1)) == (128, 128)  # operands that take no copies
+    assert tile(dict(DENSE, rows=1, k=2048, lda=2048, trans_b=1, ldb=2048)) == (16, 16)
+    assert tile({}) == (32, 64)
+    for nothing in ({"groups": 0}, {"rows": 0}, {"n": 0}):
+        assert tile(nothing) == (0, 0)
+    with pytest.raises(gdy.GdyError):
+        tile({"k": -1})
+    r, c, d = ctypes.c_int32(), ctypes.c_int32(), filled(gdy.IntegerDesc(), INTEGER, {})
+    r, c, d = ctypes.byref(r), ctypes.byref(c), ctypes.byref(d)
+    fn = ctx.lib.gdy_integer_tile
+    assert fn(None, d, r, c) == INVALID and fn(ctx.h, None, r, c) == INVALID
+    assert fn(ctx.h, d, None, c) == INVALID and fn(ctx.h, d, r, None) == INVALID
