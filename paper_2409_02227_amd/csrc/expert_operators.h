@@ -346,19 +346,23 @@ gdy_status validate_integer(gdy_ctx* ctx, const gdy_integer& g, const gdy_epilog
 
 // What a tile of such a product costs, in us: start + step for each 128 bytes of K where it has a CU to itself, share +
 // share_step where tiles fill the CUs.  Fitted to 244 products of 16 to 4096 rows, N = 1024 to 8192, K = 512 to 8192 and 1,
-// 8 and 32 groups (any: 132 of odd sizes), silu and a bias: their choices take 1.8% (any: 1.6%) more than the fastest
-// tile of each on average, 28% (21%) at most; the fp8 products' rule took 7% and 38%.
+// 8 and 32 groups (any: 132 of odd sizes), silu and a bias: their choices take 1.7% (any: 1.6%) more than the fastest
+// tile of each on average, 34% (21%) at most; the fp8 products' rule took 7% and 38%.
 struct IntegerTileCost {
   int tile, bm, bn;
   bool copies;  // both operands take copies
   double start, step, share, share_step;  // share 0: a CU holds one at a time
 };
 const IntegerTileCost kIntegerTiles[] = {
-    {INT_256, 256, 256, true, 13.36, 1.169, 0, 0},          {INT_256, 128, 256, true, 8.81, 0.776, 0, 0},
-    {INT_64x128, 64, 128, true, 5.85, 0.430, 3.63, 0.319},  {INT_64, 64, 64, true, 4.91, 0.303, 2.56, 0.219},
-    {INT_32x64, 32, 64, true, 4.72, 0.230, 1.43, 0.163},    {INT_FEW, 16, 16, true, 4.98, 0.096, 1.65, 0.096},
-    {INT_ANY_128, 128, 128, false, 8.89, 1.161, 7.74, 0.810}, {INT_ANY_64x128, 64, 128, false, 6.87, 0.797, 5.46, 0.587},
-    {INT_ANY_32x128, 32, 128, false, 5.63, 0.601, 3.95, 0.452}, {INT_ANY_32x64, 32, 64, false, 4.91, 0.439, 2.63, 0.325}};
+    {INT_256, 256, 256, true, 13.36, 1.169, 0, 0},
+    {INT_64x128, 64, 128, true, 5.85, 0.430, 3.63, 0.319},
+    {INT_64, 64, 64, true, 4.91, 0.303, 2.56, 0.219},
+    {INT_32x64, 32, 64, true, 4.72, 0.230, 1.43, 0.163},
+    {INT_FEW, 16, 16, true, 4.98, 0.096, 1.65, 0.096},
+    {INT_ANY_128, 128, 128, false, 8.89, 1.161, 7.74, 0.810},
+    {INT_ANY_64x128, 64, 128, false, 6.87, 0.797, 5.46, 0.587},
+    {INT_ANY_32x128, 32, 128, false, 5.63, 0.601, 3.95, 0.452},
+    {INT_ANY_32x64, 32, 64, false, 4.91, 0.439, 2.63, 0.325}};
 
 // Groups' sizes are unknown here: their row tiles as group_rows_tile counts them.
 const IntegerTileCost& integer_tile_of(const gdy_ctx* ctx, const gdy_integer& g, bool copies) {
@@ -368,14 +372,22 @@ const IntegerTileCost& integer_tile_of(const gdy_ctx* ctx, const gdy_integer& g,
   double best_t = 0;
   for (const IntegerTileCost& c : kIntegerTiles) {
     if (c.copies != copies || (c.tile == INT_FEW && !g.trans_b)) continue;
-    const double rows = groups <= 1 ? std::ceil((double)g.rows / c.bm) : groups / (1.0 - std::exp(-c.bm / avg));
-    const double n = rows * (double)((g.n + c.bn - 1) / c.bn) / cus, alone = c.start + c.step * steps;
+    auto tiles = [&](int bm) {  // a CU's
+      const double rows = groups <= 1 ? std::ceil((double)g.rows / bm) : groups / (1.0 - std::exp(-bm / avg));
+      return rows * (double)((g.n + c.bn - 1) / c.bn) / cus;
+    };
+    const double n = tiles(c.bm), alone = c.start + c.step * steps;
     double t;
     if (c.share > 0) {
       t = std::max(alone, std::ceil(n - 0.01) * (c.share + c.share_step * steps));
-    } else {  // a last wave of up to half the CUs runs as halves of 256-row tiles
-      const double full = std::floor(n), rest = n - full;
-      t = alone * (full + (rest == 0 ? 0.0 : c.bm == 256 && rest <= 0.5 ? 0.65 : 1.0));
+    } else {  // integer_tile_256's order: whole tiles, then those of 128 rows on the CUs that are free
+      const double rest = 2 * n - tiles(128), whole = n - rest, full = std::floor(whole), last = whole - full;
+      const double behind = rest - (1.0 - last);  // that start when the last whole ones end
+      t = alone * (full + (last == 0                ? 0.65 * std::ceil(rest)
+                           : 2 * last + rest <= 1.0 ? 0.65
+                           : behind <= 0            ? 1.0
+                           : behind <= 1.0 - last   ? 1.3
+                                                    : 1.0 + 0.65 * std::ceil(behind)));
     }
     if (!best || t < best_t) best = &c, best_t = t;
   }
@@ -435,7 +447,8 @@ gdy_status launch_integer(gdy_ctx* ctx, const gdy_integer& g, const gdy_epilogue
   a.bm = tile.bm;
   a.max_slots = (int32_t)(grouped ? max_row_tiles(g.rows, groups, a.bm) : (g.rows + a.bm - 1) / a.bm);
   const int64_t tn = (g.n + kern.bn - 1) / kern.bn;
-  const int64_t halves = a.bm == 256 ? a.xcd_cus / 2 : 0;  // workgroups for the last tiles' other halves
+  // of an XCD: the last tiles' other halves, and its short tiles are rounded up by themselves
+  const int64_t halves = a.bm == 256 ? a.xcd_cus / 2 + 1 : 0;
   const int64_t grid = (((int64_t)a.max_slots * tn + kXcds - 1) / kXcds + halves) * kXcds;
   if (grid * kern.threads > UINT32_MAX)  // threads of a launch
     return fail(ctx, GDY_ERR_UNSUPPORTED, "integer: a grid of %lld workgroups", (long long)grid);

@@ -328,7 +328,7 @@ const void* route_slots_kernel(bool few);
 constexpr int kQuantMost = 4;
 const void* quantize_kernel(int dt, int held, bool whole);
 // Products of 8-bit integers by the type of C (null: no such tile).  For operands that both take copies: 256 x 256
-// tiles (also as 128 rows), smaller ones, and kSkinnyRows rows with B stored N x K; for any operands INT_ANY_*.
+// tiles, smaller ones, and kSkinnyRows rows with B stored N x K; for any operands INT_ANY_*.
 enum : int {
   INT_256, INT_64x128, INT_64, INT_32x64, INT_FEW, INT_ANY_128, INT_ANY_64x128, INT_ANY_32x128, INT_ANY_32x64
 };

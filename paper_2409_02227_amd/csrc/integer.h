@@ -160,42 +160,103 @@ template <int DT> struct IntegerEpi : GroupEpi {
   }
 };
 
-// The tile of C that this workgroup computes, in tiles of bm x bn rows; false: none.  halves:
-// whether the last tiles run as halves of 128 rows (grouped_rows).
-template <int DT>
-__device__ __forceinline__ bool integer_tile(const KGroup& g, int bm, int bn, bool halves, IntegerEpi<DT>& e) {
+// The tile's place and extent.
+template <int DT> __device__ __forceinline__ bool place_tile(const KGroup& g, int e, int lo, int m0, int m, int n0, int bn,
+                                                             IntegerEpi<DT>& ep) {
+  ep.e = uniform(e), ep.row = uniform(lo + m0), ep.n0 = uniform(n0);
+  ep.m = uniform(m), ep.n = uniform(min(bn, g.n - n0));
+  ep.slot = 0, ep.os = OutSize<DT>::v, ep.over_k = false;
+  return ep.m > 0;
+}
+
+// The tile of C that this workgroup computes, in tiles of bm x bn rows; false: none.  Each XCD takes a contiguous
+// run of them (grouped_rows).
+template <int DT> __device__ __forceinline__ bool integer_tile(const KGroup& g, int bm, int bn, IntegerEpi<DT>& ep) {
   const int tn = (g.n + bn - 1) / bn;
   const int total = (g.offsets ? total_slots(g.offsets, g.groups, g.rows, bm, g.max_slots) : (g.rows + bm - 1) / bm) * tn;
-  const int per = (total + kXcds - 1) / kXcds;
-  int j = (int)blockIdx.x / kXcds, half = -1;
-  if (halves) {
-    const int rest = per % g.xcd_cus;
-    if (2 * rest <= g.xcd_cus && j >= per - rest) {
-      half = (j - (per - rest)) & 1;
-      j = per - rest + (j - (per - rest)) / 2;
-    }
-  }
+  const int per = (total + kXcds - 1) / kXcds, j = (int)blockIdx.x / kXcds;
   const int id = ((int)blockIdx.x & (kXcds - 1)) * per + j;
   if (j >= per || id >= total) return false;
   GroupSlot s = {0, 0, g.rows, 0};
   if (g.offsets && !find_slot(g.offsets, g.groups, g.rows, bm, id / tn, s)) return false;
   int ti, tj;
   group_tile(id - s.first * tn, (s.count + bm - 1) / bm, tn, ti, tj);
-  const int m0 = ti * bm + (half > 0 ? 128 : 0);
-  e.e = uniform(s.e), e.row = uniform(s.lo + m0), e.n0 = uniform(tj * bn);
-  e.m = uniform(min(half >= 0 ? 128 : bm, s.count - m0)), e.n = uniform(min(bn, g.n - tj * bn));
-  e.slot = 0, e.os = OutSize<DT>::v, e.over_k = false;
-  return e.m > 0;
+  return place_tile(g, s.e, s.lo, ti * bm, min(bm, s.count - ti * bm), tj * bn, bn, ep);
+}
+
+// The same in 256 x 256 tiles, of which a CU holds one.  What is left of a group behind its 256-row tiles runs as a tile
+// of 128 rows where that holds it (a "short" one, 0.65 of a whole one's time); every XCD runs those behind its whole
+// ones, so that they fill the CUs which the last of these leave (8192 rows in 16 groups of 206 to 1901 x 4096, K = 2048:
+// 104 us with each group's tiles next to each other, 97.6 this way).  Where all of them find a CU the last whole tiles run
+// as halves of 128 rows too.
+__device__ __forceinline__ int whole_tiles(int rows) { return (rows + 127) / 256; }
+__device__ __forceinline__ int short_tiles(int rows) { return (rows + 255) / 256 - (rows + 127) / 256; }
+
+template <int DT> __device__ __forceinline__ bool integer_tile_256(const KGroup& g, IntegerEpi<DT>& ep) {
+  const int tn = (g.n + 255) / 256, lane = threadIdx.x & 63;
+  int whole = 0, rest = 0;  // row tiles
+  if (g.offsets) {
+    for (int e0 = 0; e0 < g.groups; e0 += 64) {
+      const int c = group_rows(g.offsets, g.groups, g.rows, e0 + lane).count;
+      whole += __builtin_amdgcn_readlane(wave_scan(whole_tiles(c)), 63);
+      rest += __builtin_popcountll(__ballot(short_tiles(c) != 0));
+    }
+    whole = min(whole, g.max_slots);
+    rest = min(rest, g.max_slots - whole);
+  } else {
+    whole = whole_tiles(g.rows), rest = short_tiles(g.rows);
+  }
+  whole *= tn, rest *= tn;
+  const int xcd = (int)blockIdx.x & (kXcds - 1);
+  const int per = (whole + kXcds - 1) / kXcds, per_short = (rest + kXcds - 1) / kXcds;
+  const int last = per % g.xcd_cus, halved = 2 * last + per_short <= g.xcd_cus ? last : 0;
+  int j = (int)blockIdx.x / kXcds, half = -1;
+  bool is_short = false;
+  if (j >= per + halved) {
+    is_short = true;
+    j -= per + halved;
+    if (j >= per_short) return false;
+  } else if (j >= per - halved) {
+    half = (j - (per - halved)) & 1;
+    j = per - halved + (j - (per - halved)) / 2;
+  }
+  const int id = xcd * (is_short ? per_short : per) + j;
+  if (id >= (is_short ? rest : whole)) return false;
+  const int slot = id / tn;
+  int e = 0, lo = 0, count = g.rows, first = 0;
+  if (g.offsets) {
+    int before = 0;
+    bool found = false;
+    for (int e0 = 0; e0 < g.groups && !found; e0 += 64) {
+      const GroupRows r = group_rows(g.offsets, g.groups, g.rows, e0 + lane);
+      const int t = is_short ? short_tiles(r.count) : whole_tiles(r.count), s = before + wave_scan(t);
+      const uint64_t past = __ballot(s > slot);
+      if (past) {
+        const int l = (int)__builtin_ctzll(past);
+        found = true, e = e0 + l;
+        lo = __builtin_amdgcn_readlane(r.lo, l), count = __builtin_amdgcn_readlane(r.count, l);
+        first = __builtin_amdgcn_readlane(s - t, l);
+      }
+      before = __builtin_amdgcn_readlane(s, 63);
+    }
+    if (!found) return false;
+  }
+  int ti, tj;
+  if (is_short) {
+    ti = whole_tiles(count), tj = id - slot * tn;
+  } else {
+    group_tile(id - first * tn, whole_tiles(count), tn, ti, tj);
+  }
+  const int m0 = ti * 256 + (half > 0 ? 128 : 0);
+  return place_tile(g, e, lo, m0, min(half >= 0 ? 128 : 256, count - m0), tj * 256, 256, ep);
 }
 
 template <int DT, int TB, class T>
 __global__ void __launch_bounds__(T::NT, T::NT == 512 ? 2 : T::LDS > 80 * 1024 ? 1 : 2) integer_rows(KInteger q) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDS];
   const KGroup& g = q.g;
-  constexpr bool P = T::BN == 256;  // the 256 x 256 kernel has 128-row tiles too
-  const int bm = P ? g.bm : T::BM;
   IntegerEpi<DT> e;
-  if (!integer_tile<DT>(g, bm, T::BN, P && bm == 256, e)) return;
+  if (!(T::BM == 256 ? integer_tile_256<DT>(g, e) : integer_tile<DT>(g, T::BM, T::BN, e))) return;
   const uint8_t* a = g.a + (int64_t)e.row * g.lda;
   const uint8_t* b = g.b + e.e * g.stride_b + (TB == 1 ? (int64_t)e.n0 * g.ldb : (int64_t)e.n0);
   T::run(tile_args<DT, 0, TB>(g, a, b, e.m, e.n, g.k), (lds_u8*)smem, e);
@@ -208,7 +269,7 @@ __global__ void __launch_bounds__(512) integer_few(KInteger q) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[T::LDS];
   const KGroup& g = q.g;
   IntegerEpi<DT> e;
-  if (!integer_tile<DT>(g, T::BM, T::BN, false, e)) return;
+  if (!integer_tile<DT>(g, T::BM, T::BN, e)) return;
   T::tile(g.a + (int64_t)e.row * g.lda, g.b + e.e * g.stride_b + (int64_t)e.n0 * g.ldb, g.lda, g.ldb, e.m, e.n, g.k, e, 0,
           0, (lds_u8*)smem);
 }
