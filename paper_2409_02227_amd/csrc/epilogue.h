@@ -261,41 +261,138 @@ template <int DT> __device__ __forceinline__ f32x4 load_bias4(const EpiOut& o, i
     return b;
   }
 }
-// The scales of row i and of columns j .. j + 3 (products of 8-bit integers; reads past the
-// matrix return 0).
-template <int DT> __device__ __forceinline__ float row_scale(const EpiOut& o, int i) {
-  if constexpr (!IsInt8<DT>::v) return 1.0f;
-  else {
-    if (!o.row_scales) return 1.0f;
-    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(o.row_scales, o.m * 4), i * 4, 0, 0));
-  }
-}
-template <int DT> __device__ __forceinline__ f32x4 load_scales4(const EpiOut& o, int j) {
-  if constexpr (!IsInt8<DT>::v) return f32x4{1.0f, 1.0f, 1.0f, 1.0f};
-  else {
-    if (!o.col_scales) return f32x4{1.0f, 1.0f, 1.0f, 1.0f};
-    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(o.col_scales, o.n * 4), j * 4, 0, 0));
-  }
-}
-// A sum of 8-bit integers' products, from its bits, times its scales, plus the bias.
-__device__ __forceinline__ float scaled_int(float bits, float rs, float cs, float b) {
-  return __builtin_fmaf((float)__builtin_bit_cast(int, bits) * rs, cs, b);
-}
 template <int DT> __device__ __forceinline__ f32x4 linear_sums(f32x4 x, float scale, f32x4 b) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) x[q] = DT == DT_FP8 ? __builtin_fmaf(x[q], scale, b[q]) : x[q] + b[q];
   return x;
 }
-template <int DT>
-__device__ __forceinline__ u32x2 linear4(f32x4 x, float scale, f32x4 b, float rs = 1.0f, f32x4 cs = f32x4{}) {
-  if constexpr (IsInt8<DT>::v) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] = scaled_int(x[q], rs, cs[q], b[q]);
-  } else {
-    x = linear_sums<DT>(x, scale, b);
-  }
+template <int DT> __device__ __forceinline__ u32x2 linear4(f32x4 x, float scale, f32x4 b) {
+  x = linear_sums<DT>(x, scale, b);
   return u32x2{to_out2<Row8<DT>::OT>(x[0], x[1]), to_out2<Row8<DT>::OT>(x[2], x[3])};
 }
+
+// ---- products of 8-bit integers -------------------------------------------------
+// The scales of row i and of columns j .. j + 3 (reads past the matrix return 0).
+__device__ __forceinline__ float row_scale(const EpiOut& o, int i) {
+  if (!o.row_scales) return 1.0f;
+  return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(o.row_scales, o.m * 4), i * 4, 0, 0));
+}
+__device__ __forceinline__ f32x4 load_scales4(const EpiOut& o, int j) {
+  if (!o.col_scales) return f32x4{1.0f, 1.0f, 1.0f, 1.0f};
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(o.col_scales, o.n * 4), j * 4, 0, 0));
+}
+// A sum of 8-bit integers' products, from its bits, times its scales, plus the bias.
+__device__ __forceinline__ float scaled_int(float bits, float rs, float cs, float b) {
+  return __builtin_fmaf((float)__builtin_bit_cast(int, bits) * rs, cs, b);
+}
+// The bias and the scales of eight columns.
+template <int DT> struct Columns {
+  float b[8];
+  f32x4 cs[2];
+  __device__ __forceinline__ void load(const EpiOut& o, int col) {
+    load_bias<DT>(o, col, b);
+    cs[0] = load_scales4(o, col), cs[1] = load_scales4(o, col + 4);
+  }
+};
+
+// Eight sums of a row to C, plus `res` where there is one.
+template <int DT>
+__device__ __forceinline__ void put_ints(f32x4 lo, f32x4 hi, float rs, const Columns<DT>& of, int act, const Row8<DT>& res,
+                                         bool add, Rsrc rc, int off, bool vec, int left) {
+  float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+  for (int q = 0; q < 8; ++q) x[q] = scaled_int(x[q], rs, of.cs[q / 4][q & 3], of.b[q]);
+  apply_values(x, act);
+  if (add) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] += res.get(q);
+  }
+  Row8<DT> w;
+  w.set(x);
+  w.store(rc, off, vec, left);
+}
+template <int DT>  // from LDS
+__device__ __forceinline__ void put_ints(const lds_u8* src, float rs, const Columns<DT>& of, int act, const Row8<DT>& res,
+                                         bool add, Rsrc rc, int off, bool vec, int left) {
+  typedef const __attribute__((address_space(3))) f32x4* Src;
+  put_ints<DT>(*(Src)src, *(Src)(src + 16), rs, of, act, res, add, rc, off, vec, left);
+}
+
+// A wave's sums, rounded, to the rows of a tile in LDS (C of 16 bits).
+template <int DT, int PITCH, int FN, int FM>
+__device__ __forceinline__ void put_packed(const EpiOut& o, const f32x4 (&acc)[FN][FM], lds_u8* tile, int row, int col,
+                                           int lane) {
+  const int r0 = row + (lane & 15), c0 = col + 4 * (lane >> 4);
+  auto all = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const f32x4 b = load_bias4<DT>(o, c0 + j * 16), cs = load_scales4(o, c0 + j * 16);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const float rs = row_scale(o, r0 + i * 16);
+        float x[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] = f(scaled_int(acc[j][i][q], rs, cs[q], b[q]));
+        *(__attribute__((address_space(3))) u32x2*)(tile + (r0 + i * 16) * PITCH + (c0 + j * 16) * 2) =
+            u32x2{to_out2<Row8<DT>::OT>(x[0], x[1]), to_out2<Row8<DT>::OT>(x[2], x[3])};
+      }
+    }
+  };
+  if (o.act == ACT_NONE) all([](float x) { return x; });
+  else by_act(o.act, [&](auto a) { all([](float x) { return act_value<decltype(a)::value>(x); }); });
+}
+
+// The end of a tile of go_kernel_u.h, for a wave's block of R rows x WC columns.
+template <int DT, int R, int WC> struct IntEnd {
+  static constexpr int OS = OutSize<DT>::v, LPR = WC / 8, RP = 64 / LPR;  // lanes a row, rows a pass
+  static constexpr int PART = R < 32 ? R : 32, PASSES = PART / RP;        // rows in LDS together
+  static constexpr int PITCH = WC * 4 + 16, BYTES = PART * PITCH;
+  static_assert(R % PART == 0 && PART % RP == 0, "whole passes");
+
+  // block: the wave's BYTES of LDS
+  template <int FN, int FM>
+  static __device__ __forceinline__ void run(const EpiOut& o, const f32x4 (&acc)[FN][FM], lds_u8* block, int row, int col,
+                                             int lane) {
+    float rs[R / RP];
+    Columns<DT> of;
+#pragma unroll
+    for (int p = 0; p < R / RP; ++p) rs[p] = row_scale(o, row + p * RP + lane / LPR);
+    of.load(o, col + (lane % LPR) * 8);
+    const Rsrc rc = make_rsrc(o.c, o.c_bytes), rr = make_rsrc(o.res, o.res ? ((o.m - 1) * o.ldr + o.n) * OS : 0);
+    const int c = col + (lane % LPR) * 8, left = o.n - c;
+    const bool whole = __ballot(left > 0 && left < 8) == 0;  // every lane has all its columns inside C, or none
+    const bool c_vec = whole && (OS == 4 || o.c_vec), r_vec = whole && (OS == 4 || o.res_vec);
+#pragma unroll
+    for (int h = 0; h < R / PART; ++h) {
+      if (row + h * PART >= o.m) break;
+      auto at = [&](int p, int ld) {
+        const int r = row + h * PART + p * RP + lane / LPR;
+        return r < o.m && left > 0 ? (r * ld + c) * OS : kOutOfRange;
+      };
+      auto inside = [&](int p) { return row + h * PART + p * RP + lane / LPR < o.m ? left : 0; };
+      Row8<DT> res[PASSES];
+      if (o.res) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) res[p].load(rr, at(p, o.ldr), r_vec, inside(p));
+      }
+#pragma unroll
+      for (int i = 0; i < PART / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          *(__attribute__((address_space(3))) f32x4*)(block + (i * 16 + (lane & 15)) * PITCH + (j * 16 + 4 * (lane >> 4)) * 4) =
+              acc[j][h * (PART / 16) + i];
+      // the wave's own sums, in LDS in the order of its instructions
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p)
+        put_ints<DT>(block + (p * RP + lane / LPR) * PITCH + (lane % LPR) * 32, rs[h * PASSES + p], of, o.act, res[p],
+                     o.res != nullptr, rc, at(p, o.ldc), c_vec, inside(p));
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next sums
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+};
 
 // What a wave does with blocks of R rows x WC columns of a tile's sums, one after
 // another: the caller lays a block's sums into the wave's LDS, PITCH bytes a row, and
@@ -316,7 +413,6 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
   bool grad;
   bool whole;     // every lane of the wave has all its columns inside C, or none
   float b[8], sum[8];
-  f32x4 cs[2];    // 8-bit integers: the columns' scales
 
   __device__ __forceinline__ EpiWave(const EpiOut& out, int lane_) : o(out), lane(lane_) {
     rc = make_rsrc(o.c, o.c_bytes);
@@ -330,7 +426,6 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
     left = o.n - col;
     whole = __ballot(left > 0 && left < 8) == 0;
     load_bias<DT>(o, col, b);
-    if constexpr (IsInt8<DT>::v) cs[0] = load_scales4<DT>(o, col), cs[1] = load_scales4<DT>(o, col + 4);
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum[q] = 0.0f;
   }
@@ -343,15 +438,11 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
     if (grad) aux.load(ra, at(in, row, o.ldaux), whole && (OS == 4 || o.aux_vec), left);
   }
 
-  // Eight sums of a row to C (rs: its row_scale()).
-  __device__ __forceinline__ void finish(bool in, int row, float (&x)[8], const Row8<DT>& res, const Row8<DT>& aux,
-                                         float rs) {
+  // Eight sums of a row to C.
+  __device__ __forceinline__ void finish(bool in, int row, float (&x)[8], const Row8<DT>& res, const Row8<DT>& aux) {
     Row8<DT> w;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      if constexpr (IsInt8<DT>::v) x[q] = scaled_int(x[q], rs, cs[q / 4][q & 3], b[q]);
-      else x[q] = DT == DT_FP8 ? __builtin_fmaf(x[q], o.scale, b[q]) : x[q] + b[q];
-    }
+    for (int q = 0; q < 8; ++q) x[q] = DT == DT_FP8 ? __builtin_fmaf(x[q], o.scale, b[q]) : x[q] + b[q];
     if (grad) {
       float z[8];
       aux.get(z);
@@ -387,12 +478,9 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
     for (int u0 = 0; u0 < PASSES; u0 += AHEAD) {
       Row8<DT> res[AHEAD], aux[AHEAD];
       const int r0 = lane / LPR + u0 * RP;
-      float rs[AHEAD];
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
+      for (int u = 0; u < AHEAD; ++u)
         load_inputs(r0 + u * RP < count && left > 0, m0 + r0 + u * RP, res[u], aux[u]);
-        rs[u] = row_scale<DT>(o, m0 + r0 + u * RP);
-      }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         const int r = r0 + u * RP;
@@ -400,7 +488,7 @@ template <int DT, int R, int WC, int ROWS_AHEAD> struct EpiWave {
         const f32x4 lo = *(const __attribute__((address_space(3))) f32x4*)p;
         const f32x4 hi = *(const __attribute__((address_space(3))) f32x4*)(p + 16);
         float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        finish(r < count && left > 0, m0 + r, x, res[u], aux[u], rs[u]);
+        finish(r < count && left > 0, m0 + r, x, res[u], aux[u]);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next block's sums
@@ -472,7 +560,7 @@ __global__ void __launch_bounds__(256) split_reduce_ep(KLaunch L, KEpis E) {
           if (q < x.left)
             for (int s = 0; s < S; ++s) v[q] += P[s * plane + q];
       }
-      x.finish(true, row, v, res, aux, 1.0f);
+      x.finish(true, row, v, res, aux);
     }
     if (x.o.part) {
       x.put_sums((lds_u8*)smem, tid / Wave::LPR, BN, (tid % Wave::LPR) * 8);

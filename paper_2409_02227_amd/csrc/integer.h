@@ -11,7 +11,6 @@ namespace gdy {
 
 // A tile and where its results go: as GroupEpi, with the scales.
 template <int DT> struct IntegerEpi : GroupEpi {
-  static constexpr bool linear = OutSize<DT>::v == 2;
   __device__ __forceinline__ EpiOut operator()(int item, int tile_row) const {
     EpiOut o = GroupEpi::operator()(item, tile_row);
     typedef const __attribute__((address_space(4))) KInteger* Ptr;
@@ -34,24 +33,6 @@ template <int DT> struct IntegerEpi : GroupEpi {
     else by_quadrants(o, acc, half, smem);
   }
 
-  // Eight sums of a row to C.
-  static __device__ __forceinline__ void put8(const lds_u8* src, float rs, const f32x4 (&cs)[2], const float (&b)[8], int act,
-                                              const Row8<DT>* res, Rsrc rc, int off, bool vec, int left) {
-    const f32x4 lo = *(const __attribute__((address_space(3))) f32x4*)src;
-    const f32x4 hi = *(const __attribute__((address_space(3))) f32x4*)(src + 16);
-    float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-#pragma unroll
-    for (int q = 0; q < 8; ++q) x[q] = scaled_int(x[q], rs, cs[q / 4][q & 3], b[q]);
-    apply_values(x, act);
-    if (res) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) x[q] += res->get(q);
-    }
-    Row8<DT> w;
-    w.set(x);
-    w.store(rc, off, vec, left);
-  }
-
   // 128 columns at a time, 16 lanes a row, a wave 32 rows, four of them a pass.
   __device__ __forceinline__ void by_rows(const EpiOut& o, const f32x4 (&acc)[2][2][2][4], bool half, lds_u8* smem) const {
     constexpr int OS = OutSize<DT>::v, PITCH = 128 * 4 + 16, PASSES = 8;
@@ -60,15 +41,12 @@ template <int DT> struct IntegerEpi : GroupEpi {
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), wm = wave >> 2, wn = wave & 3;
     const Rsrc rc = make_rsrc(o.c, o.c_bytes), rr = make_rsrc(o.res, ((o.m - 1) * o.ldr + o.n) * OS);
     const int r0 = wave * 32 + (lane >> 4), c0 = (lane & 15) * 8;
-    float rs[PASSES], b[2][8];
-    f32x4 cs[2][2];
+    float rs[PASSES];
+    Columns<DT> of[2];
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) rs[p] = row_scale<DT>(o, r0 + 4 * p);
+    for (int p = 0; p < PASSES; ++p) rs[p] = row_scale(o, r0 + 4 * p);
 #pragma unroll
-    for (int hb = 0; hb < 2; ++hb) {
-      cs[hb][0] = load_scales4<DT>(o, hb * 128 + c0), cs[hb][1] = load_scales4<DT>(o, hb * 128 + c0 + 4);
-      load_bias<DT>(o, hb * 128 + c0, b[hb]);
-    }
+    for (int hb = 0; hb < 2; ++hb) of[hb].load(o, hb * 128 + c0);
     const bool live = wave * 32 < o.m;  // some of the wave's rows lie inside C
 #pragma unroll
     for (int hb = 0; hb < 2; ++hb) {
@@ -103,7 +81,7 @@ template <int DT> struct IntegerEpi : GroupEpi {
         if (p0) load(p0);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
-          put8(smem + (r0 + 4 * (p0 + u)) * PITCH + c0 * 4, rs[p0 + u], cs[hb], b[hb], o.act, &res[u], rc,
+          put_ints<DT>(smem + (r0 + 4 * (p0 + u)) * PITCH + c0 * 4, rs[p0 + u], of[hb], o.act, res[u], true, rc,
                at(p0 + u, o.ldc), c_vec, inside(p0 + u));
       }
     }
@@ -118,14 +96,13 @@ template <int DT> struct IntegerEpi : GroupEpi {
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), wm = wave >> 2, wn = wave & 3;
     const Rsrc rc = make_rsrc(o.c, o.c_bytes);
     const int r0 = wm * 64 + (lane >> 2), c0 = wn * 32 + (lane & 3) * 8;  // of quadrant 0
-    float rs[2][PASSES], b[2][8];
-    f32x4 cs[2][2];
+    float rs[2][PASSES];
+    Columns<DT> of[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int p = 0; p < PASSES; ++p) rs[h][p] = row_scale<DT>(o, r0 + h * 128 + 16 * p);
-      cs[h][0] = load_scales4<DT>(o, c0 + h * 128), cs[h][1] = load_scales4<DT>(o, c0 + h * 128 + 4);
-      load_bias<DT>(o, c0 + h * 128, b[h]);
+      for (int p = 0; p < PASSES; ++p) rs[h][p] = row_scale(o, r0 + h * 128 + 16 * p);
+      of[h].load(o, c0 + h * 128);
     }
     auto place = [&](int q) { return smem + (q & 1) * (8 * BLOCK) + wave * BLOCK; };
     // quadrant q: columns q / 2, rows q % 2
@@ -151,8 +128,8 @@ template <int DT> struct IntegerEpi : GroupEpi {
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
         const int row = r0 + (q & 1) * 128 + 16 * p;
-        put8(place(q) + ((lane >> 2) + 16 * p) * PITCH + (lane & 3) * 32, rs[q & 1][p], cs[q >> 1], b[q >> 1], o.act, nullptr,
-             rc, row < o.m && left > 0 ? (row * o.ldc + c0 + (q >> 1) * 128) * OS : kOutOfRange, vec, row < o.m ? left : 0);
+        put_ints<DT>(place(q) + ((lane >> 2) + 16 * p) * PITCH + (lane & 3) * 32, rs[q & 1][p], of[q >> 1], o.act, Row8<DT>(), false, rc,
+             row < o.m && left > 0 ? (row * o.ldc + c0 + (q >> 1) * 128) * OS : kOutOfRange, vec, row < o.m ? left : 0);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next sums in this place
       __builtin_amdgcn_wave_barrier();

@@ -71,6 +71,17 @@ template <int DT, int TB> struct Skinny {
     const int a0 = i * lda_b + g * (16 * AV);
     const int b0 = TB == 1 ? i * ldb_b + g * (16 * AV) : g * KROWS * ldb_b + i * 4 * ES;
 
+    // 8-bit integers have scales to wait for: (1, 2048, 2048) 4.5 us, with these loads behind the loop 5.1
+    Columns<DT> columns;
+    float rs = 1.0f;
+    if constexpr (IsInt8<DT>::v) {
+      if (wave == 0) {
+        const EpiOut o = ep(item, 0);
+        columns.load(o, n0 + (tid % (BN / 8)) * 8);
+        rs = row_scale(o, tid / (BN / 8));
+      }
+    }
+
     f32x4 acc[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -141,6 +152,32 @@ template <int DT, int TB> struct Skinny {
       }
     }
     __syncthreads();
+    if constexpr (IsInt8<DT>::v) {
+      constexpr int LPR = BN / 8;  // lanes a row
+      static_assert(BM * LPR <= 64, "the first wave finishes the rows");
+      const int row = tid / LPR, c = n0 + (tid % LPR) * 8;
+      if (wave == 0 && row < m) {
+        const EpiOut o = ep(item, 0);
+        const int left = o.n - c;
+        const bool whole = __ballot(left > 0 && left < 8) == 0;
+        if (left <= 0) return;
+        constexpr int OS = OutSize<DT>::v;
+        Row8<DT> res;
+        if (o.res)
+          res.load(make_rsrc(o.res, ((o.m - 1) * o.ldr + o.n) * OS), (row * o.ldr + c) * OS, whole && (OS == 4 || o.res_vec),
+                   left);
+        const lds_u8* at = smem + row * PITCH + (tid % LPR) * 32;
+        i32x4 lo = {0, 0, 0, 0}, hi = lo;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          lo += *(const __attribute__((address_space(3))) i32x4*)(at + w * (BM * PITCH));
+          hi += *(const __attribute__((address_space(3))) i32x4*)(at + w * (BM * PITCH) + 16);
+        }
+        put_ints<DT>(__builtin_bit_cast(f32x4, lo), __builtin_bit_cast(f32x4, hi), rs, columns, o.act, res, o.res != nullptr,
+                     make_rsrc(o.c, o.c_bytes), (row * o.ldc + c) * OS, whole && (OS == 4 || o.c_vec), left);
+      }
+      return;
+    }
     typedef EpiWave<DT, BM, BN, 1> Epi;
     constexpr int USED = BM * Epi::LPR;  // threads that finish rows: 32 or 128
     const int row = tid / Epi::LPR;
@@ -156,17 +193,11 @@ template <int DT, int TB> struct Skinny {
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          const f32x4 l = *(const lds_f32x4*)(at + w * (BM * PITCH)), h = *(const lds_f32x4*)(at + w * (BM * PITCH) + 16);
-          if constexpr (IsInt8<DT>::v) {
-            lo = __builtin_bit_cast(f32x4, __builtin_bit_cast(i32x4, lo) + __builtin_bit_cast(i32x4, l));
-            hi = __builtin_bit_cast(f32x4, __builtin_bit_cast(i32x4, hi) + __builtin_bit_cast(i32x4, h));
-          } else {
-            lo += l;
-            hi += h;
-          }
+          lo += *(const lds_f32x4*)(at + w * (BM * PITCH));
+          hi += *(const lds_f32x4*)(at + w * (BM * PITCH) + 16);
         }
         float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        x.finish(true, row, v, res, aux, row_scale<DT>(x.o, row));
+        x.finish(true, row, v, res, aux);
       }
       if (part) x.put_sums(smem + TABLE, row, BN, (tid % Epi::LPR) * 8);
     }
