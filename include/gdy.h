@@ -556,8 +556,8 @@ gdy_status gdy_execute_quantize(gdy_ctx* ctx, const gdy_quantize* op, void* hip_
  * The sums are exact (32-bit integers; k is at most 131071); each of the products with the
  * scales, and the rest, is fp32.  With offsets, a product grouped by expert over rows, as
  * gdy_execute_grouped: the rows offsets[e] .. offsets[e+1] - 1 of A and C belong to group e, with
- * its own B, column scales and bias; offsets are clamped to 0 .. rows, rows of no group left as
- * they were.  Without, one product of all rows (groups and the strides are ignored).  The epilogue
+ * its own B, column scales and bias; offsets do not decrease and are clamped to 0 .. rows; rows of no
+ * group are left as they were.  Without, one product of all rows (groups and the strides are ignored).  The epilogue
  * may hold a bias, an activation and a residual (R may be C itself; stride_bias counts
  * between groups).  Allocates nothing and uses no workspace.  A group's B, and 512 rows of A and
  * of C, must end within 2 GiB.  Non-finite scales give what the formulas give.

@@ -356,3 +356,33 @@ def test_every_tile(ctx, tb, pad):
         assert found == {(256, 256), (64, 128), (64, 64), (32, 64)} | ({(16, 16)} if tb else set()), found
     else:
         assert found == {(128, 128), (64, 128), (32, 128), (32, 64)}, found
+
+
+@pytest.mark.parametrize("tb", [0, 1])
+def test_short_tiles_behind_whole_ones(ctx, tb):
+    """Groups' ends of one row to a whole tile, in more groups than a wave's lanes; each way that the last tiles run."""
+    ends = [1, 127, 128, 129, 255, 256, 257, 383, 384, 385, 0, 640]
+    for groups, n, scale in ((100, 608, 1), (9, 2064, 1), (70, 1008, 1), (13, 1040, 3)):
+        counts = [scale * ends[(7 * e) % len(ends)] for e in range(groups)]
+        offsets = [3]
+        for c in counts:
+            offsets.append(offsets[-1] + c)
+        x = Product("bf16", offsets[-1] + 5, offsets, n, 128, tb, "relu", "own", groups == 9, pad=16)
+        assert ctx.int8_tile(x.product) == (256, 256)
+        run(ctx, x)
+
+
+def test_groups_past_four_gib(ctx):
+    """The B of groups 2^31 bytes apart."""
+    groups, n, k = 4, 96, 64
+    gen = torch.Generator().manual_seed(9)
+    whole = torch.zeros(3 * 2 ** 31 + n * k, dtype=torch.int8, device="cuda")
+    b = whole.as_strided((groups, n, k), (2 ** 31, k, 1))
+    b.copy_(codes(gen, n, k, items=groups))
+    a = codes(gen, 40, k)
+    c = torch.zeros(40, n, device="cuda")
+    ctx.execute_int8(gdy.Int8(a, b, c, offsets=torch.arange(0, 41, 10, dtype=torch.int32).cuda(), trans_b=1))
+    torch.cuda.synchronize()
+    for e in range(groups):
+        want = a[10 * e:10 * e + 10].double() @ b[e].double().t()
+        assert torch.equal(c[10 * e:10 * e + 10].double(), want), e
