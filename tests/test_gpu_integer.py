@@ -137,7 +137,7 @@ def test_dense(ctx, dtype, rows, n, k, tb):
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("tb", [0, 1])
 def test_dense_large_tiles(ctx, dtype, tb):
-    """Tiles of 256 x 256 and 128 x 256, whole and ragged, in both ends (with a bias alone, and with more)."""
+    """Tiles of 256 x 256, whole and of 128 rows, in both ends (with a residual and without)."""
     for rows, n, k in ((2048, 2304, 256), (4000, 4100, 128), (8192, 256, 384), (1408, 4096, 144)):
         run(ctx, Product(dtype, rows, None, n, k, tb, bias="own"))
         run(ctx, Product(dtype, rows, None, n, k, tb, "gelu", "own", True, inplace=True))
@@ -386,3 +386,18 @@ def test_groups_past_four_gib(ctx):
     for e in range(groups):
         want = a[10 * e:10 * e + 10].double() @ b[e].double().t()
         assert torch.equal(c[10 * e:10 * e + 10].double(), want), e
+
+
+@pytest.mark.parametrize("tb", [0, 1])
+def test_no_k_on_large_tiles(ctx, tb):
+    """The bias and the residual alone, dense and by group; A and B have no addresses."""
+    bias, res = torch.randn(2304, device="cuda"), torch.randn((2100, 2304), device="cuda")
+    for groups in (0, 3):
+        a = torch.zeros((2100, 0), dtype=torch.int8, device="cuda")
+        b = torch.zeros(((groups,) if groups else ()) + ((2304, 0) if tb else (0, 2304)), dtype=torch.int8, device="cuda")
+        c = torch.zeros((2100, 2304), device="cuda")
+        offsets = torch.tensor([0, 700, 700, 2100], dtype=torch.int32).cuda() if groups else None
+        for residual in (None, res):
+            ctx.execute_int8(gdy.Int8(a, b, c, offsets=offsets, trans_b=tb, epilogue=gdy.Epilogue(bias, "none", residual)))
+            torch.cuda.synchronize()
+            assert torch.equal(c, bias + (0 if residual is None else residual)), (groups, residual is None)
