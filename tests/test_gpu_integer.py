@@ -400,4 +400,4 @@ def test_no_k_on_large_tiles(ctx, tb):
         for residual in (None, res):
             ctx.execute_int8(gdy.Int8(a, b, c, offsets=offsets, trans_b=tb, epilogue=gdy.Epilogue(bias, "none", residual)))
             torch.cuda.synchronize()
-            assert torch.equal(c, bias + (0 if residual is None else residual)), (groups, residual is None)
+            assert (c == bias + (0 if residual is None else residual)).all(), (groups, residual is None)
