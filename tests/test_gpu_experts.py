@@ -543,3 +543,36 @@ def test_two_contexts_and_repeated_results(ctx):
             assert torch.equal(v, b.results()[k]), k
     finally:
         second.close()
+
+
+def test_more_rows_than_workgroups(ctx):
+    """Rows of a workgroup each, more of them than a launch has workgroups: the first are followed by others."""
+    t, n, tokens = torch.bfloat16, 2064, (1 << 21) + 5
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.empty((tokens, n), dtype=t, device="cuda").normal_(generator=gen)
+    some = torch.cat([torch.arange(16), torch.arange(tokens - 16, tokens), torch.randint(0, tokens, (200,))]).cuda()
+    q, s = torch.zeros((tokens, n), dtype=torch.int8, device="cuda"), torch.zeros(tokens, device="cuda")
+    ctx.execute_quantize(gdy.Quantize(x, q, s))
+    torch.cuda.synchronize()
+    want, scale = reference(x[some])
+    assert torch.equal(q[some].cpu(), want)
+    close(s[some], scale, EPS32 * scale, "scales")
+    assert int(torch.count_nonzero(s)) == tokens
+    del q, s
+    # backward, to the rows in reverse: out = 2 x exactly, sums of n products in fp32
+    slots = torch.arange(tokens - 1, -1, -1, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    w, dw = torch.full((tokens, 1), 2.0, device="cuda"), torch.full((tokens, 1), float("nan"), device="cuda")
+    z = torch.empty((tokens, n), dtype=t, device="cuda").normal_(generator=gen)
+    out = torch.zeros_like(x)
+    ctx.execute_scatter(gdy.Scatter(x, slots, out, w, z, dw))
+    torch.cuda.synchronize()
+    other = tokens - 1 - some
+    assert torch.equal(out[other], x[some] * 2) and not torch.isnan(dw).any()
+    a, b = x[some].double(), z[other].double()
+    close(dw[some, 0], (a * b).sum(1).cpu(), (n + 4) * EPS32 * (a * b).abs().sum(1).cpu(), "weight_grad")
+    del out
+    y = torch.zeros_like(x)
+    ctx.execute_combine(gdy.Combine(z, slots, y, None, x))
+    torch.cuda.synchronize()
+    sums = z[other].double() + x[some].double()
+    close(y[some], sums.cpu(), (half_step(t) * sums.abs() + 2 * EPS32 * (z[other].abs() + x[some].abs()).double()).cpu(), "combine")
