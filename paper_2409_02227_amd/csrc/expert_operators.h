@@ -113,7 +113,12 @@ gdy_status launch_route(gdy_ctx* ctx, const gdy_route& g, hipStream_t hs) {
       HIP_TRY(ctx, launch(route_sums_kernel(), (a.experts + 63) / 64));
     }
   }
-  HIP_TRY(ctx, launch(route_slots_kernel(few), a.parts));
+  // Few pairs and experts take a workgroup of four waves in place of 16: 64 pairs of 16 experts 3.7 us and 3.9,
+  // of 256 3.7 and 4.2.
+  const bool small = few && a.pairs <= kRouteSmall * 64;
+  const int waves = small ? kRouteSmall : kRoutePart / 64;
+  HIP_TRY(ctx, hipExtLaunchKernel(route_slots_kernel(few, waves), dim3(a.parts), dim3(waves * 64), argv, 0, hs, nullptr,
+                                  nullptr, 0));
   return GDY_OK;
 }
 

@@ -245,19 +245,20 @@ __device__ __forceinline__ void lds_in_order() {
 // a wave is ranked once; several are counted, then read and ranked again.  Without totals (route_sums) the
 // parts' counts are summed by all threads, `wide` experts next to each other.
 // The code is kept short: a call this small waits for its instructions as for its data.
-template <int EXPERTS>
-__global__ void __launch_bounds__(kRoutePart) route_slots(KRoute g) {
+template <int EXPERTS, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) route_slots(KRoute g) {
+  constexpr int PART = WAVES * 64;
   __shared__ int base[EXPERTS];
-  __shared__ uint16_t count[kRouteWaves][EXPERTS];
-  __shared__ int sums[kRouteWaves];
-  __shared__ int part_total[kRoutePart], part_before[kRoutePart];
+  __shared__ uint16_t count[WAVES][EXPERTS];
+  __shared__ int sums[WAVES];
+  __shared__ int part_total[PART], part_before[PART];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int E = g.experts;
-  const int p0 = ((int)blockIdx.x * kRouteWaves + wave) * g.steps * 64 + lane;
+  const int p0 = ((int)blockIdx.x * WAVES + wave) * g.steps * 64 + lane;
   int e = pair_expert(g, p0);
-  for (int i = tid; i < E; i += kRoutePart)
+  for (int i = tid; i < E; i += PART)
 #pragma unroll
-    for (int w = 0; w < kRouteWaves; ++w) count[w][i] = 0;
+    for (int w = 0; w < WAVES; ++w) count[w][i] = 0;
   __syncthreads();
   // the rank of a step's pair among the wave's pairs of its expert, on top of `count`
   auto rank = [&](int e) {
@@ -284,7 +285,7 @@ __global__ void __launch_bounds__(kRoutePart) route_slots(KRoute g) {
     }
   }
   // experts, `wide` at a time: counts of the waves before, of the parts before, of the experts before
-  const int wide = min(kRoutePart, g.expert_threads), rows = kRoutePart / wide;
+  const int wide = min(PART, g.expert_threads), rows = PART / wide;
   const int column = tid & (wide - 1), row = tid / wide;
   int below = 0;
 #pragma unroll 1
@@ -311,7 +312,7 @@ __global__ void __launch_bounds__(kRoutePart) route_slots(KRoute g) {
     const bool mine = row == 0 && x < E;
     if (mine) {
 #pragma unroll
-      for (int w = 0; w < kRouteWaves; ++w) {
+      for (int w = 0; w < WAVES; ++w) {
         const int c = count[w][x];
         count[w][x] = (uint16_t)total;
         total += c;
@@ -328,7 +329,7 @@ __global__ void __launch_bounds__(kRoutePart) route_slots(KRoute g) {
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
     int first = below + upto - total;
-    for (int w = 0; w < kRouteWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       if (w < wave) first += sums[w];
       below += sums[w];
     }

@@ -228,6 +228,7 @@ struct KCombine {
 // threads each.
 constexpr int kRoutePart = 1024, kRouteFew = 256, kMaxExperts = 4096;
 constexpr int kRouteMaxSteps = 63;  // parts of fewer than 2^16 pairs
+constexpr int kRouteSmall = 4;      // waves of a workgroup that is enough for all pairs
 struct KRoute {
   const void* ids;
   int32_t* slots;
@@ -323,7 +324,7 @@ const void* scatter_kernel(int dt, int mode);  // mode 0: copies (dt names the s
 const void* combine_kernel(int dt);
 const void* route_count_kernel(bool few);  // few: at most kRouteFew experts
 const void* route_sums_kernel();
-const void* route_slots_kernel(bool few);
+const void* route_slots_kernel(bool few, int waves);  // kRouteSmall waves (few alone) or those of kRoutePart
 // held: steps that a thread keeps (1, 2, or kQuantMost and more); whole: rows of whole steps.
 constexpr int kQuantMost = 4;
 const void* quantize_kernel(int dt, int held, bool whole);

@@ -260,7 +260,8 @@ __device__ __forceinline__ void u_tiles(const KArgs& args, int lwg, int nwg, lds
 #pragma unroll
             for (int i = 0; i < C::FM; ++i) {
               if constexpr (IsInt8<DT>::v) {
-                acc[j][i] = s == 0 ? M::template part<0>(bf[j], af[i], acc[j][i]) : M::template part<1>(bf[j], af[i], acc[j][i]);
+                acc[j][i] = s == 0 ? M::template part<0>(bf[j], af[i], acc[j][i])
+                                   : M::template part<1>(bf[j], af[i], acc[j][i]);
               } else if constexpr (C::ES == 4) {
                 const unsigned b = bf[j][s], a = af[i][s];  // copies: a bit cast of a vector's element takes its first
                 acc[j][i] = M::run(__builtin_bit_cast(float, b), __builtin_bit_cast(float, a), acc[j][i]);

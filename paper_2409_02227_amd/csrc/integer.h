@@ -25,7 +25,7 @@ template <int DT> struct IntegerEpi : GroupEpi {
   // through LDS, so that a lane has eight consecutive columns of a row.  All that the arithmetic reads (scales,
   // bias, the first residual rows) is on its way before the sums are laid down: with loads in front of each group of
   // rows the end of a tile took 14 us of the 44 that a tile of 8192 rows in 16 groups x 4096, K = 2048, with silu
-  // takes in all, now 10.  Tiles without a residual leave by quadrants (28.5 us for (4096, 8192, 128) with silu, by rows
+  // takes in all, now 8.  Tiles without a residual leave by quadrants (28.5 us for (4096, 8192, 128) with silu, by rows
   // 30.5), those with one by rows, whose loads and stores are of 256 bytes (45.7 us, by quadrants 49.1).
   __device__ __forceinline__ void finish(const f32x4 (&acc)[2][2][2][4], bool half, lds_u8* smem) const {
     const EpiOut o = (*this)(0, 0);
@@ -111,8 +111,8 @@ template <int DT> struct IntegerEpi : GroupEpi {
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          *(__attribute__((address_space(3))) f32x4*)(place(q) + (i * 16 + (lane & 15)) * PITCH + (j * 16 + 4 * (lane >> 4)) * 4) =
-              acc[q & 1][q >> 1][j][i];
+          *(__attribute__((address_space(3))) f32x4*)(place(q) + (i * 16 + (lane & 15)) * PITCH +
+                                                      (j * 16 + 4 * (lane >> 4)) * 4) = acc[q & 1][q >> 1][j][i];
     };
     auto done = [&](int q) { return half && (q & 1); };  // no such rows
     dump(0);
@@ -128,8 +128,9 @@ template <int DT> struct IntegerEpi : GroupEpi {
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
         const int row = r0 + (q & 1) * 128 + 16 * p;
-        put_ints<DT>(place(q) + ((lane >> 2) + 16 * p) * PITCH + (lane & 3) * 32, rs[q & 1][p], of[q >> 1], o.act, Row8<DT>(), false, rc,
-             row < o.m && left > 0 ? (row * o.ldc + c0 + (q >> 1) * 128) * OS : kOutOfRange, vec, row < o.m ? left : 0);
+        const int at = row < o.m && left > 0 ? (row * o.ldc + c0 + (q >> 1) * 128) * OS : kOutOfRange;
+        put_ints<DT>(place(q) + ((lane >> 2) + 16 * p) * PITCH + (lane & 3) * 32, rs[q & 1][p], of[q >> 1], o.act,
+                     Row8<DT>(), false, rc, at, vec, row < o.m ? left : 0);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next sums in this place
       __builtin_amdgcn_wave_barrier();

@@ -29,6 +29,9 @@ const void* gdy::route_count_kernel(bool few) {
   return few ? reinterpret_cast<const void*>(&route_count<kRouteFew>) : reinterpret_cast<const void*>(&route_count<kMaxExperts>);
 }
 const void* gdy::route_sums_kernel() { return reinterpret_cast<const void*>(&route_sums); }
-const void* gdy::route_slots_kernel(bool few) {
-  return few ? reinterpret_cast<const void*>(&route_slots<kRouteFew>) : reinterpret_cast<const void*>(&route_slots<kMaxExperts>);
+const void* gdy::route_slots_kernel(bool few, int waves) {
+#define GDY_SLOTS(EXPERTS, WAVES) reinterpret_cast<const void*>(&route_slots<EXPERTS, WAVES>)
+  if (waves == kRouteSmall) return few ? GDY_SLOTS(kRouteFew, kRouteSmall) : nullptr;
+  return few ? GDY_SLOTS(kRouteFew, kRoutePart / 64) : GDY_SLOTS(kMaxExperts, kRoutePart / 64);
+#undef GDY_SLOTS
 }

@@ -576,3 +576,13 @@ def test_more_rows_than_workgroups(ctx):
     torch.cuda.synchronize()
     sums = z[other].double() + x[some].double()
     close(y[some], sums.cpu(), (half_step(t) * sums.abs() + 2 * EPS32 * (z[other].abs() + x[some].abs()).double()).cpu(), "combine")
+
+
+@pytest.mark.parametrize("tokens,top_k,experts", [(64, 4, 256), (256, 1, 256), (256, 1, 257), (257, 1, 256), (129, 1, 64), (32, 8, 65),
+                                                   (4, 64, 200), (1, 1, 256), (63, 1, 2), (2, 1, 4096)])
+def test_route_few_pairs(ctx, tokens, top_k, experts):
+    """Around the pairs and experts that a small workgroup takes."""
+    gen = torch.Generator().manual_seed(tokens + experts)
+    ids = torch.randint(-1, experts + 1, (tokens, top_k), generator=gen)
+    check_route(ctx, ids.cuda(), experts)
+    check_route(ctx, torch.full((tokens, top_k), experts - 1, dtype=torch.int32).cuda(), experts)
