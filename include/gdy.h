@@ -462,7 +462,7 @@ gdy_status gdy_execute_act_grad(gdy_ctx* ctx, const gdy_act_grad* op, void* hip_
  * call may have the same row; slots outside 0 .. rows - 1 are none.  Rows that no slot names
  * are left as they were.  All calls are asynchronous on `hip_stream` and allocate nothing;
  * outputs may overlap nothing else but where it is said.  Leading dimensions are at most
- * 2^44, matrices of any alignment of their elements.
+ * 2^44, a matrix ends within 2^63 bytes, at any alignment of its elements.
  *
  * Routing: ids[t * ld_ids + j] is the expert of pair (t, j); ids outside 0 .. experts - 1 are none
  * (the share of another GPU, padding).  The pairs sorted by expert, those of one expert in

@@ -4,8 +4,12 @@
 
 namespace {
 
-// Leading dimensions whose byte offsets a 64-bit product holds for any row.
 bool good_ld(int64_t ld, int64_t n) { return ld >= n && ld <= kMaxStride; }
+
+// Whether 64-bit byte offsets reach the end of a matrix: 2^31 rows of 2^44 elements pass them.
+bool good_extent(int64_t rows, int64_t n, int64_t ld, int es) {
+  return rows <= 1 || ((__int128)(rows - 1) * ld + n) * es <= INT64_MAX;
+}
 
 bool row_type(int32_t t) { return t == GDY_F16 || t == GDY_BF16 || t == GDY_F32; }
 
@@ -70,6 +74,8 @@ gdy_status validate_route(gdy_ctx* ctx, const gdy_route& g) {
     if (!g.ids || !g.slots || (uintptr_t)g.slots % 4 || (uintptr_t)g.ids % g.id_bytes)
       return fail(ctx, GDY_ERR_INVALID_ARG, "route: null or unaligned ids or slots");
     if (!good_ld(g.ld_ids, g.top_k)) return fail(ctx, GDY_ERR_INVALID_ARG, "route: bad ld_ids");
+    if (!good_extent(g.tokens, g.top_k, g.ld_ids, g.id_bytes))
+      return fail(ctx, GDY_ERR_UNSUPPORTED, "route: ids past 64-bit offsets");
     ranges.push_back({matrix_range(g.ids, g.tokens, g.top_k, g.ld_ids, 1, 0, g.id_bytes), false, 0});
     ranges.push_back({matrix_range(g.slots, 1, g.tokens * g.top_k, 0, 1, 0, 4), true, 0});
   }
@@ -146,6 +152,9 @@ gdy_status validate_scatter(gdy_ctx* ctx, const gdy_scatter& g) {
     if (!g.x || !g.out || (g.weight_grad && !g.z)) return fail(ctx, GDY_ERR_INVALID_ARG, "scatter: null x, out or z");
     if (!good_ld(g.ldx, g.n) || !good_ld(g.ldo, g.n) || (g.weight_grad && !good_ld(g.ldz, g.n)))
       return fail(ctx, GDY_ERR_INVALID_ARG, "scatter: a leading dimension < n or > 2^44");
+    if (!good_extent(g.tokens, g.n, g.ldx, es) || !good_extent(g.rows, g.n, g.ldo, es) ||
+        (g.weight_grad && !good_extent(g.rows, g.n, g.ldz, es)))
+      return fail(ctx, GDY_ERR_UNSUPPORTED, "scatter: operands past 64-bit offsets");
     if (((uintptr_t)g.x | (uintptr_t)g.out | (g.weight_grad ? (uintptr_t)g.z : 0)) % es)
       return fail(ctx, GDY_ERR_UNSUPPORTED, "scatter: operands not element aligned");
     ranges.push_back({matrix_range(g.x, g.tokens, g.n, g.ldx, 1, 0, es), false, 0});
@@ -197,6 +206,9 @@ gdy_status validate_combine(gdy_ctx* ctx, const gdy_combine& g) {
   if (!g.y || (g.rows > 0 && !g.z)) return fail(ctx, GDY_ERR_INVALID_ARG, "combine: null y or z");
   if (!good_ld(g.ldy, g.n) || (g.rows > 0 && !good_ld(g.ldz, g.n)) || (g.residual && !good_ld(g.ldr, g.n)))
     return fail(ctx, GDY_ERR_INVALID_ARG, "combine: a leading dimension < n or > 2^44");
+  if (!good_extent(g.tokens, g.n, g.ldy, es) || !good_extent(g.rows, g.n, g.ldz, es) ||
+      (g.residual && !good_extent(g.tokens, g.n, g.ldr, es)))
+    return fail(ctx, GDY_ERR_UNSUPPORTED, "combine: operands past 64-bit offsets");
   if (((uintptr_t)g.y | (uintptr_t)g.residual | (g.rows > 0 ? (uintptr_t)g.z : 0)) % es)
     return fail(ctx, GDY_ERR_UNSUPPORTED, "combine: operands not element aligned");
   ranges.push_back({matrix_range(g.y, g.tokens, g.n, g.ldy, 1, 0, es), true, 1});
@@ -250,6 +262,8 @@ gdy_status validate_quantize(gdy_ctx* ctx, const gdy_quantize& g) {
     if (!g.x || !g.q) return fail(ctx, GDY_ERR_INVALID_ARG, "quantize: null x or q");
     if (!good_ld(g.ldx, g.n) || !good_ld(g.ldq, g.n))
       return fail(ctx, GDY_ERR_INVALID_ARG, "quantize: a leading dimension < n or > 2^44");
+    if (!good_extent(g.rows, g.n, g.ldx, es) || !good_extent(out_rows, g.n, g.ldq, 1))
+      return fail(ctx, GDY_ERR_UNSUPPORTED, "quantize: operands past 64-bit offsets");
     if ((uintptr_t)g.x % es) return fail(ctx, GDY_ERR_UNSUPPORTED, "quantize: x not element aligned");
     ranges.push_back({matrix_range(g.x, g.rows, g.n, g.ldx, 1, 0, es), false, 0});
     ranges.push_back({matrix_range(g.q, out_rows, g.n, g.ldq, 1, 0, 1), true, 0});

@@ -299,6 +299,44 @@ def test_quantize_checks(ctx, kw, want):
     assert status(ctx, ctx.lib.gdy_execute_quantize, ctypes.byref(filled(gdy.QuantizeDesc(), QUANTIZE, kw)), None) == want
 
 
+# Rows of 2^40 bytes: offsets of 2^23 of them end below 2^63, of one more at 2^63 and past it.  The second of two rows
+# of 2^44 elements lies inside 64 bits whatever the type.
+LAST, PAST = 1 << 23, (1 << 23) + 1
+
+
+@pytest.mark.parametrize("op,kw,want", [
+    ("route", {"tokens": 1 << 20, "ld_ids": 1 << 40}, OK),
+    ("route", {"tokens": (1 << 20) + 1, "ld_ids": 1 << 40}, UNSUPPORTED),
+    ("route", {"tokens": (1 << 20) + 1, "ld_ids": 1 << 40, "id_bytes": 4}, OK),
+    ("route", {"tokens": 1 << 23, "ld_ids": 1 << 44}, UNSUPPORTED),
+    ("scatter", {"tokens": LAST, "ldx": 1 << 39}, OK), ("scatter", {"tokens": PAST, "ldx": 1 << 39}, UNSUPPORTED),
+    ("scatter", {"rows": LAST, "ldo": 1 << 39}, OK), ("scatter", {"rows": PAST, "ldo": 1 << 39}, UNSUPPORTED),
+    ("scatter", {"rows": LAST, "ldz": 1 << 39}, OK), ("scatter", {"rows": PAST, "ldz": 1 << 39}, UNSUPPORTED),
+    ("scatter", {"rows": PAST, "ldz": 1 << 39, "z": None, "weight_grad": None}, OK),
+    ("scatter", {"tokens": PAST, "ldx": 1 << 38, "type": gdy.F32}, UNSUPPORTED),
+    ("scatter", {"tokens": (1 << 31) - 4097, "top_k": 1, "ldx": 1 << 44}, UNSUPPORTED), ("scatter", {"tokens": 2, "ldx": 1 << 44}, OK),
+    ("combine", {"tokens": LAST, "ldy": 1 << 39}, OK), ("combine", {"tokens": PAST, "ldy": 1 << 39}, UNSUPPORTED),
+    ("combine", {"rows": LAST, "ldz": 1 << 39}, OK), ("combine", {"rows": PAST, "ldz": 1 << 39}, UNSUPPORTED),
+    ("combine", {"tokens": LAST, "ldr": 1 << 39}, OK), ("combine", {"tokens": PAST, "ldr": 1 << 39}, UNSUPPORTED),
+    ("combine", {"tokens": PAST, "ldr": 1 << 39, "residual": None}, OK), ("combine", {"rows": 0, "ldz": 1 << 62}, OK),
+    ("quantize", {"rows": LAST, "ldx": 1 << 39}, OK), ("quantize", {"rows": PAST, "ldx": 1 << 39}, UNSUPPORTED),
+    ("quantize", {"out_rows": LAST, "ldq": 1 << 40}, OK), ("quantize", {"out_rows": PAST, "ldq": 1 << 40}, UNSUPPORTED),
+    ("quantize", dict(PLAIN, rows=PAST, ldq=1 << 40), UNSUPPORTED), ("quantize", {"rows": PAST, "ldx": 1 << 39, "n": 0}, OK),
+])
+def test_matrices_past_64_bit_offsets(ctx, op, kw, want):
+    """Where the last row's byte offset would not fit a signed 64-bit product the call is refused, however few of the
+    rows are named."""
+    base, struct = {"route": (ROUTE, gdy.RouteDesc), "scatter": (SCATTER, gdy.ScatterDesc), "combine": (COMBINE, gdy.CombineDesc),
+                    "quantize": (QUANTIZE, gdy.QuantizeDesc)}[op]
+    d = filled(struct(), base, kw)
+    far = {"ldx": "x", "ldo": "out", "ldz": "z", "ldy": "y", "ldr": "residual", "ldq": "q", "ld_ids": "ids"}
+    apart = [name for ld, name in far.items() if ld in kw]
+    for i, (name, kind) in enumerate(struct._fields_):  # 2^40 bytes for each operand, the one with rows far apart last
+        if kind is ctypes.c_void_p and getattr(d, name):
+            setattr(d, name, 1 << 50 if name in apart else (i + 1) << 40)
+    assert status(ctx, getattr(ctx.lib, "gdy_execute_" + op), ctypes.byref(d), None) == want
+
+
 INTEGER = dict(rows=64, n=96, k=128, c_type=gdy.BF16, trans_b=0, groups=4, offsets=at(0), a=at(1), lda=128, b=at(2), ldb=96,
                stride_b=128 * 96, row_scales=at(3), col_scales=at(4), stride_col_scales=96, c=at(5), ldc=96)
 DENSE = dict(offsets=None, groups=0, stride_b=0, stride_col_scales=0)
