@@ -66,7 +66,9 @@ __global__ void __launch_bounds__(COLS * LANES) group_sums(GroupSums s) {
   } else {
     first = first_slot(s.offsets, s.groups, s.rows, s.bm, e);
     const GroupRows g = group_rows(s.offsets, s.groups, s.rows, e);
-    count = min((g.count + s.bm - 1) / s.bm, max(s.max_slots - first, 0));
+    // decreasing offsets: groups behind the last tile, or so many tiles before them that the sum turns negative
+    count = first < 0 || first >= s.max_slots ? 0 : min((g.count + s.bm - 1) / s.bm, s.max_slots - first);
+    first = count ? first : 0;
   }
   column_sums<COLS, LANES>(s.part + (int64_t)first * s.per * s.n, s.out + e * s.stride, s.n, count * s.per, col, lds);
 }

@@ -280,6 +280,20 @@ def test_act_grad(ctx, dtype, rows, n, act):
             close(dz2[covered.cuda()], x.c[covered], x.c_bound[covered], ("dz", dtype, rows, n, act))
 
 
+def test_act_grad_of_more_tiles_than_31_bits(ctx):
+    """Decreasing offsets that give every row to every other group: their tiles together are 2^32, and no group's sums
+    are read from in front of the workspace.  The first group's sums, exact here, and those of groups without rows are right."""
+    rows, groups, n = 1 << 26, 4096, 8
+    dy = torch.zeros((rows, n), dtype=torch.bfloat16, device="cuda")
+    dy[::1 << 16] = torch.arange(n, device="cuda").to(torch.bfloat16)
+    offsets = torch.tensor([0, rows] * (groups // 2) + [0], dtype=torch.int32, device="cuda")
+    sums = torch.full((groups, n), float("nan"), device="cuda")
+    ctx.execute_act_grad(gdy.ActGrad(dy, None, None, sums, "none", offsets))
+    torch.cuda.synchronize()
+    assert torch.equal(sums[0].cpu(), torch.arange(n) * 1024.0)
+    assert (sums[1] == 0).all() and (sums[3:] == 0).all()  # no rows, behind the last tile, past 31 bits
+
+
 def test_act_grad_infinities(ctx):
     z = torch.tensor([[float("inf"), float("-inf"), 70.0, -70.0, 0.0]] * 2, dtype=torch.float32, device="cuda")
     dy = torch.full_like(z, 3.0)
