@@ -401,3 +401,47 @@ def test_no_k_on_large_tiles(ctx, tb):
             ctx.execute_int8(gdy.Int8(a, b, c, offsets=offsets, trans_b=tb, epilogue=gdy.Epilogue(bias, "none", residual)))
             torch.cuda.synchronize()
             assert (c == bias + (0 if residual is None else residual)).all(), (groups, residual is None)
+
+
+def bounds_of_many(groups, rows, kind):
+    """Offsets of more groups than a wave has lanes.  spread: rows all over, empty groups on both sides of the first
+    64; behind: no rows in the first 64; across: rows in the first and last group of each 64 alone; back: as
+    spread, with an offset past the first 64 that decreases."""
+    gen = torch.Generator().manual_seed(groups + rows)
+    if kind == "behind":
+        ends = [2] * 65 + sorted(torch.randint(2, rows, (groups - 65,), generator=gen).tolist())
+        return ends + [rows - 1]
+    if kind == "across":
+        own = [e for e in range(groups) if e % 64 in (0, 63)]
+        ends, at = [1], 1
+        for e in range(groups):
+            at = min(at + (1 + (rows - 4) // len(own) if e in own else 0), rows - 1)
+            ends.append(at)
+        return ends
+    inner = torch.randint(3, rows - 2, (groups - 1,), generator=gen)
+    ends = [3] + sorted(inner.tolist()) + [rows - 2]
+    ends[63] = ends[62]  # group 62 is empty, and 64 where it is not the last
+    if groups > 65:
+        ends[65] = ends[64]
+    if kind == "back":
+        ends[groups - 1] = ends[groups - 2] - min(5, ends[groups - 2])
+    return ends
+
+
+MANY = [  # groups, rows, n, k, and the tiles of operands that take copies (B stored K x N, N x K) and of others
+    (65, 100, 80, 144, (32, 64), (16, 16), (32, 64)), (130, 100, 64, 1024, (32, 64), (16, 16), (32, 64)),
+    (130, 300, 256, 512, (32, 64), (32, 64), (32, 128)), (257, 300, 256, 512, (64, 128), (64, 128), (32, 128)),
+    (65, 3000, 2064, 80, (64, 128), (64, 128), (64, 128)), (257, 100, 80, 144, (32, 64), (16, 16), (32, 64))]
+
+
+@pytest.mark.parametrize("groups,rows,n,k,nn,nt,others", MANY)
+@pytest.mark.parametrize("kind", ["spread", "behind", "across", "back"])
+@pytest.mark.parametrize("tb", [0, 1])
+def test_small_tiles_of_many_groups(ctx, groups, rows, n, k, nn, nt, others, kind, tb):
+    """More groups than a wave reads at a time, each with few rows, on the tiles that such products take."""
+    offsets = bounds_of_many(groups, rows, kind)
+    assert len(offsets) == groups + 1 and (kind == "back") == (offsets != sorted(offsets))
+    for pad, tile in ((0, nt if tb else nn), (3, others)):
+        x = Product("bf16", rows, offsets, n, k, tb, "silu" if pad else "none", "own", kind == "spread", pad=pad)
+        assert ctx.int8_tile(x.product) == tile
+        run(ctx, x)
