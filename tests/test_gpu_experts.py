@@ -586,3 +586,121 @@ def test_route_few_pairs(ctx, tokens, top_k, experts):
     ids = torch.randint(-1, experts + 1, (tokens, top_k), generator=gen)
     check_route(ctx, ids.cuda(), experts)
     check_route(ctx, torch.full((tokens, top_k), experts - 1, dtype=torch.int32).cuda(), experts)
+
+
+class Bounded:
+    """A value in 64 bits and how far an fp32 computation of it may be off, element by element.  A sum of K products in
+    any order is off by (K + 4) * 2^-24 of their absolute sum, one operation by 2^-24 of its result, on top of what the
+    operands bring along."""
+
+    def __init__(self, v, e=None):
+        self.v, self.e = v, torch.zeros_like(v) if e is None else e
+
+    def most(self):
+        return self.v.abs() + self.e
+
+    def __matmul__(self, o):
+        k = self.v.shape[1]
+        return Bounded(self.v @ o.v, self.most() @ o.most() - self.v.abs() @ o.v.abs() +
+                       (k + 4) * EPS32 * (self.most() @ o.most()))
+
+    def __mul__(self, o):
+        return Bounded(self.v * o.v, self.most() * o.most() - (self.v * o.v).abs() + EPS32 * self.most() * o.most())
+
+    def t(self):
+        return Bounded(self.v.t(), self.e.t())
+
+    def __getitem__(self, i):
+        return Bounded(self.v[i], self.e[i])
+
+
+def forward64(x, w1, w2, w, res, ids):
+    """y of the layer by its formula, in 64 bits."""
+    y = [res]
+    for e in range(w1.shape[0]):
+        i, j = (ids == e).nonzero(as_tuple=True)
+        z = torch.nn.functional.silu(x[i] @ w1[e]) @ w2[e]
+        y.append(torch.zeros_like(res).index_put((i,), w[i, j][:, None] * z, accumulate=True))
+    return sum(y)
+
+
+def bounded_layer(x):
+    """The results of a Layer in fp32 with their bounds.  silu: its slope is below 1.2, its second derivative below 0.6,
+    and the kernels' are within 2^-17 of the value and 2^-30, and within 2^-17 of what a slope multiplies."""
+    leaf = lambda v: Bounded(v.double().cpu())  # noqa: E731
+    a, w1, w2, w, dy, res = (leaf(v) for v in (x.x, x.w1, x.w2, x.w, x.dy, x.res))
+    ids = x.ids.cpu()
+    parts = {k: ([], []) for k in ("y", "dx")}
+    out = {"dw": Bounded(torch.zeros_like(w.v)), "dw1": Bounded(torch.zeros_like(w1.v)), "dw2": Bounded(torch.zeros_like(w2.v))}
+    for e in range(w1.v.shape[0]):
+        i, j = (ids == e).nonzero(as_tuple=True)
+        if not len(i):
+            continue
+        xs, g = a[i], dy[i]
+        z1 = xs @ w1[e]
+        s = torch.sigmoid(z1.v)
+        h = Bounded(z1.v * s)
+        h.e = 1.2 * z1.e + 2.0 ** -17 * (h.v.abs() + 1.2 * z1.e) + 2.0 ** -30
+        z2 = h @ w2[e]
+        weight = w[i, j]
+        weight = Bounded(weight.v[:, None], weight.e[:, None])
+        dz2 = weight * g
+        dot = Bounded(g.v, g.e) * z2
+        dw = Bounded(dot.v.sum(1), dot.e.sum(1) + (dot.v.shape[1] + 4) * EPS32 * dot.most().sum(1))
+        dh = dz2 @ w2[e].t()
+        slope = s * (1 + z1.v * (1 - s))
+        dz1 = Bounded(dh.v * slope, 1.2 * dh.e + dh.most() * (0.6 * z1.e + 2.0 ** -17) + 2.0 ** -30)
+        dxs = dz1 @ w1[e].t()
+        out["dw"].v[i, j], out["dw"].e[i, j] = dw.v, dw.e
+        for name, l, r in (("dw2", h, dz2), ("dw1", xs, dz1)):
+            p = l.t() @ r
+            out[name].v[e], out[name].e[e] = p.v, p.e
+        for name, p in (("y", weight * z2), ("dx", dxs)):
+            parts[name][0].append(i), parts[name][1].append(p)
+    for name, start in (("y", res), ("dx", Bounded(torch.zeros_like(a.v)))):
+        v, e, most = start.v.clone(), start.e.clone(), start.v.abs()
+        for i, p in zip(*parts[name]):
+            v.index_put_((i,), p.v, accumulate=True), e.index_put_((i,), p.e, accumulate=True)
+            most = most.index_put((i,), p.most(), accumulate=True)
+        out[name] = Bounded(v, e + (w.v.shape[1] + 4) * EPS32 * most)
+    return out
+
+
+@pytest.mark.parametrize("tokens,top_k,experts,n,hidden", [(40, 2, 6, 64, 96), (37, 3, 8, 96, 160), (1, 1, 1, 5, 7), (130, 5, 5, 33, 130)])
+def test_layer_in_fp32(ctx, tokens, top_k, experts, n, hidden):
+    """Forward and backward in fp32 against autograd in 64 bits, each element within the roundings that lead to it."""
+    x = Layer(ctx, tokens, top_k, experts, n, hidden, tokens, torch.float32)
+    x.run()
+    torch.cuda.synchronize()
+    ref = x.reference()
+    for name, b in bounded_layer(x).items():
+        assert torch.allclose(b.v, ref[name], rtol=1e-10, atol=1e-11), name  # the bounds' values are autograd's
+        print(name, float((getattr(x, name).double().cpu() - b.v).abs().max()), float(b.e.max()), flush=True)
+        close(getattr(x, name), b.v, b.e, (name, tokens, top_k, experts, n, hidden))
+
+
+def test_layer_gradients_along_themselves(ctx):
+    """Slopes along directions that are mostly the gradient's own, so that they are as large as it: (L(v + h u) - L(v - h
+    u)) / 2h of the layer in 64 bits, h = 2^-16, against <g, u> of the operators in fp32, which may be off by the
+    roundings of g's elements.  The difference itself is off by less than 2^-18 of |g|, which is above 2^4: by h^2 / 6 = 2^-34.6
+    times a third derivative below 2^16 (a unit step changes no z by more than 2^4, the norm of a row of x, their squares' sum
+    by 2^8, and what they are weighted with is below 2^4), and by 2^-53 of L < 2^12 over h."""
+    x = Layer(ctx, 40, 2, 6, 64, 96, 9, torch.float32)
+    x.run()
+    torch.cuda.synchronize()
+    bounds = bounded_layer(x)
+    leaves = {k: getattr(x, k).double().cpu() for k in ("x", "w1", "w2", "w")}
+    res, dy, ids = x.res.double().cpu(), x.dy.double().cpu(), x.ids.cpu()
+    gen = torch.Generator().manual_seed(1)
+    h = 2.0 ** -16
+    for leaf, grad in (("x", "dx"), ("w", "dw"), ("w1", "dw1"), ("w2", "dw2")):
+        g = getattr(x, grad).double().cpu()
+        r = torch.randn(g.shape, generator=gen, dtype=torch.float64)
+        u = g / g.norm() + 0.25 * r / r.norm()
+        u /= u.norm()
+        ends = [float((forward64(**dict(leaves, **{leaf: leaves[leaf] + sign * h * u}), res=res, ids=ids) * dy).sum())
+                for sign in (1, -1)]
+        slope, mine = (ends[0] - ends[1]) / (2 * h), float((g * u).sum())
+        bound = float((bounds[grad].e * u.abs()).sum()) + 2.0 ** -18 * float(g.norm())
+        print(leaf, slope, mine, bound, float(g.norm()), flush=True)
+        assert mine > 0.9 * float(g.norm()) and abs(slope - mine) <= bound, (leaf, slope, mine, bound)
