@@ -110,10 +110,12 @@ gdy_status launch_route(gdy_ctx* ctx, const gdy_route& g, hipStream_t hs) {
     return hipExtLaunchKernel(kernel, dim3(grid), dim3(kRoutePart), argv, 0, hs, nullptr, nullptr, 0);
   };
   if (!alone) {
-    a.counts = (int32_t*)ctx->split_ws;  // at most 261 parts x 4096 experts: 4 MiB, and the totals
+    a.counts = (int32_t*)ctx->split_ws;  // at most 261 parts x 4096 experts and the totals: 4.1 MiB
     HIP_TRY(ctx, launch(route_count_kernel(few), a.parts));
-    // Every workgroup of the last launch reads the counts, or a launch of its own sums them: 131072 pairs of 128
-    // experts (16384 counts) 9.8 and 10.8 us, of 256 12.2 and 10.9, of 4096 83 and 20.
+    // Every workgroup of the last launch reads the counts, or a launch of its own sums them: 131072 pairs of 96 experts
+    // (12288 counts) 9.8 and 10.7 us, of 128 (16384) 9.7 and 10.6, of 160 (20480) 12.2 and 10.9, of 256 12.1 and 10.8, of
+    // 4096 83 and 20; 2^20 pairs of 64 (16384) 17.2 and 19.2, of 128 19.7 and 19.3; 16384 pairs of 1024 (16384) 11.3 and
+    // 11.6, of 2048 15.9 and 13.6.
     if (a.parts * a.experts > 16384) {
       a.totals = a.counts + (int64_t)a.parts * a.experts;
       HIP_TRY(ctx, launch(route_sums_kernel(), (a.experts + 63) / 64));
@@ -285,8 +287,8 @@ gdy_status launch_quantize(gdy_ctx* ctx, const gdy_quantize& g, hipStream_t hs) 
   a.n = (int32_t)g.n;
   a.top_k = g.top_k;
   a.out_rows = (int32_t)g.out_rows;
-  // Rows of more than 4096 elements take 1024 threads where there are few of them ((512, 16384) bf16 12.3 us on 256 and
-  // 10.5 on 1024; (4096, 8192) 28.8, on 512 29.6).
+  // Rows of more than 4096 elements take up to 1024 threads where there are few of them: (64, 16384) bf16 6.6 us on 256
+  // and 4.8 on 1024, (512, 16384) 9.8 and 9.2, (1024, 8192) 9.2 and 8.8, (4096, 8192) 23.1 and 26.4.
   const int64_t units = (g.n + 15) / 16;
   const int threads = units > kRowThreads && units <= 2048 && g.rows <= 4 * ctx->cus ? 1024 : kRowThreads;
   while ((1 << a.tpr_log) < threads && (1 << a.tpr_log) < units) ++a.tpr_log;

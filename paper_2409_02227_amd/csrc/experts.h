@@ -2,9 +2,12 @@
 // each expert (route), tokens' rows to them (scatter) and back (combine), with the
 // gradients of both.
 //
-// Scatter and combine are bound by memory.  Both go by tokens: a token's row is read (or
-// written) once and its top_k rows of the other side next to it, so that nothing but the
-// slots says where rows lie, no atomics are needed and every sum has a fixed order.
+// Scatter and combine are bound by memory.  Both go by tokens: a token's row is written once
+// (combine), or read once for every four of its pairs (scatter), and its top_k rows of the other
+// side next to it, so that nothing but the slots says where rows lie, no atomics are needed
+// and every sum has a fixed order.  Scatter's later reads come out of the caches: 4096 rows of
+// 4096 bf16 to eight experts each take 60.7 us, 8192 rows to two 40.4, both 5.0 TB/s counting one
+// read of each row.
 #pragma once
 #include "grouped.h"
 #include "rows.h"

@@ -2,10 +2,11 @@
 // 127 x / max |x| rounded to the nearest integer.
 //
 // Bound by memory: a row is read once, kept in registers between its maximum and its codes
-// (rows of more than 16384 elements are read again), 16 elements a thread and step, and
-// written 16 bytes a lane.  (4096, 8192) 24.6 us in bf16, 4.1 TB/s, and 32.4 in fp32, 5.2 TB/s: the 16-bit types still
-// show their arithmetic (with the exact rounding of fp32 28.8, by three operations a code more 30.4).  The next row's
-// loads in front of a row's arithmetic: 34, for the waves that their registers cost.
+// (up to 16384 elements, in launches of at most four rows a CU up to 32768; of longer rows the rest
+// is read again), 16 elements a thread and step, and written 16 bytes a lane.  (4096, 8192) 22.7 to 24.6 us in bf16, 4.1
+// to 4.4 TB/s, and 32.4 in fp32, 5.2 TB/s: the 16-bit types still show their arithmetic (with the exact rounding of
+// fp32 28.8, by three operations a code more 30.4).  The next row's loads in front of a row's arithmetic: 34, for the
+// waves that their registers cost.
 //
 // The quotient is rounded exactly.  x times the fp32 of 127 / max is off by at most 127 * 2^-24 <
 // 1e-5, so only values that close to a half can fall on its wrong side.  Those of fp32 rows compare 127 x -
